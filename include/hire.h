@@ -261,6 +261,47 @@ int hire_softmax_step(const hire_softmax_layer* L, const void* x, int B, int k, 
 int topk_select(const float* scores, int B, int N, int k, int flags, int32_t* idx_out, float* val_out,
                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Dense gated FFN layers ----------------------------------------------------------------------------------------
+ * A layer whose units are all used, by any number of tokens (decode steps, prompts, training):
+ *   g_bj = <wg_j, x_b>,  u_bj = <wu_j, x_b>,  h_bj = a(g_bj) u_bj,  y_b = sum_j h_bj v_j
+ * with a = max(g, 0), g / (1 + exp(-g)), or 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))). */
+#define HIRE_ACT_RELU 0
+#define HIRE_ACT_SILU 1
+#define HIRE_ACT_GELU 2
+
+#define HIRE_GATED_MAX_TOKENS (1 << 20)
+#define HIRE_GATED_MAX_WIDTH (1 << 20) /* largest d_model and d_ff */
+
+typedef struct hire_gated_layer {
+  int d_model;     /* d; multiple of 8 */
+  int d_ff;        /* multiple of 8 */
+  const void* wg;  /* bf16 [d_ff, d_model], row j = wg_j (the gate) */
+  const void* wu;  /* bf16 [d_ff, d_model], row j = wu_j */
+  const void* w2u; /* bf16 [d_ff, d_model], row j = v_j */
+  int act;         /* HIRE_ACT_* */
+} hire_gated_layer;
+
+/* x, y: bf16 [T, d_model], 1 <= T <= HIRE_GATED_MAX_TOKENS; y is rounded once from fp32 sums over h, and h is rounded
+ * to bf16 between the two layers.  g, u, h: bf16 [T, d_ff] each, 16-byte aligned: what hire_gated_ffn_backward reads; all
+ * three, or all NULL where no backward pass follows.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on
+ * invalid arguments, never 0 on valid ones), 256-byte aligned; no initialisation needed, and hire_workspace_init does no
+ * harm.  x and y must not overlap.  HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
+size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T);
+int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* g, void* u, void* h,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sum(dy * y), dy bf16 [T, d_model], from what the forward call left in g, u and h:
+ *   dh = <v_j, dy_b>;  dg = dh u a'(g);  du = dh a(g)   (a'(0) = 0 for HIRE_ACT_RELU)
+ *   dw2u_j = sum_b h_bj dy_b;  dwg_j = sum_b dg_bj x_b;  dwu_j = sum_b du_bj x_b;  dx_b = sum_j dg_bj wg_j + du_bj wu_j
+ * dx bf16 [T, d_model]; dwg, dwu, dw2u bf16 [d_ff, d_model]: each is written whole (nothing is added to what was there),
+ * and each may be NULL, at least one not.  Sums are fp32, rounded once; dg and du are rounded to bf16 in between.
+ * Results are the same from call to call.  Alignment, workspace (hire_gated_ffn_backward_workspace_bytes) and errors as
+ * for the forward call. */
+size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T);
+int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* g, const void* u, const void* h,
+                            const void* dy, void* dx, void* dwg, void* dwu, void* dw2u, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

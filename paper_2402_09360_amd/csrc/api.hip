@@ -14,6 +14,15 @@
 // hipGetSymbolAddress returns (static_scratch below), never through the name.
 static __device__ __align__(256) unsigned char scratch[HIRE_STATIC_SCRATCH_BYTES];
 
+namespace hire {
+
+hipError_t& last_launch_error() {
+  static thread_local hipError_t error = hipSuccess;
+  return error;
+}
+
+}  // namespace hire
+
 namespace {
 
 using namespace hire;
@@ -256,13 +265,12 @@ int check_common(int d, int N, int B, int k, int kprime, int scorer_kind, const 
   return HIRE_OK;
 }
 
-thread_local hipError_t g_last_hip_error = hipSuccess;
 
 #define HIRE_TRY(expr)                 \
   do {                                 \
     const hipError_t e_ = (expr);      \
     if (e_ != hipSuccess) {            \
-      g_last_hip_error = e_;           \
+      last_launch_error() = e_;        \
       return HIRE_ELAUNCH;             \
     }                                  \
   } while (0)
@@ -581,7 +589,7 @@ void hire_force_exact_stage(int on) { g_force_exact_stage = on; }
 
 void hire_set_stage_events(void** events) { g_stage_events = reinterpret_cast<hipEvent_t*>(events); }
 
-const char* hire_last_launch_error(void) { return hipGetErrorString(g_last_hip_error); }
+const char* hire_last_launch_error(void) { return hipGetErrorString(last_launch_error()); }
 
 size_t hire_pack_int4_bytes(int rows, int cols) {
   if (rows < 1 || cols < 32 || cols % 32 != 0) return 0;
@@ -751,14 +759,14 @@ static int static_scratch(void** out) {
   int dev = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess || dev < 0 || dev >= kMaxDevices) {
-    g_last_hip_error = e != hipSuccess ? e : hipErrorInvalidDevice;
+    last_launch_error() = e != hipSuccess ? e : hipErrorInvalidDevice;
     return HIRE_ELAUNCH;
   }
   void* p = ptr_of_device[dev].load(std::memory_order_acquire);
   if (p == nullptr) {
     e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch));
     if (e != hipSuccess || p == nullptr) {
-      g_last_hip_error = e != hipSuccess ? e : hipErrorInvalidSymbol;
+      last_launch_error() = e != hipSuccess ? e : hipErrorInvalidSymbol;
       return HIRE_ELAUNCH;
     }
     ptr_of_device[dev].store(p, std::memory_order_release);  // threads that race here store the same address

@@ -470,4 +470,26 @@ struct FfnShardBuffers {
 hipError_t launch_ffn_shard_batch(const FfnShardArgs& a, const FfnShardBuffers& f, hipStream_t s);
 hipError_t launch_ffn_shard_reduce(const FfnShardArgs& a, hipStream_t s);  // y = their sum
 
+
+// ---- gated_ffn.hip: dense gated FFN layers, any number of tokens ----------------
+constexpr int kActRelu = 0, kActSilu = 1, kActGelu = 2;
+struct GatedLayer {
+  int d, d_ff, act;
+  const uint16_t* wg;   // bf16 [d_ff, d] each
+  const uint16_t* wu;
+  const uint16_t* w2u;
+};
+// Bytes of the fp32 parts of a product with a T x d result and k = segments * d_ff (0: it is not split).
+size_t gated_part_bytes(int T, int d, int d_ff, int segments);
+// y [T, d]; h [T, d_ff]; g, u (both or neither) likewise: what the backward pass reads.
+hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, uint16_t* h, uint16_t* g,
+                                uint16_t* u, float* part, hipStream_t s);
+// dx, dwg, dwu, dw2u: any may be null; dg, du [T, d_ff] scratch.
+hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const uint16_t* g, const uint16_t* u,
+                                 const uint16_t* h, const uint16_t* dy, uint16_t* dx, uint16_t* dwg, uint16_t* dwu,
+                                 uint16_t* dw2u, uint16_t* dg, uint16_t* du, float* part, hipStream_t s);
+
+// The HIP error behind the calling thread's most recent HIRE_ELAUNCH (api.hip).
+hipError_t& last_launch_error();
+
 }  // namespace hire

@@ -117,6 +117,21 @@ _lib.topk_select.restype = _i
 _lib.topk_select.argtypes = [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]
 
 
+
+class _GatedLayer(C.Structure):
+    _fields_ = [("d_model", C.c_int), ("d_ff", C.c_int), ("wg", C.c_void_p), ("wu", C.c_void_p), ("w2u", C.c_void_p),
+                ("act", C.c_int)]
+
+
+for _name in ("hire_gated_ffn_workspace_bytes", "hire_gated_ffn_backward_workspace_bytes"):
+    getattr(_lib, _name).restype = _sz
+    getattr(_lib, _name).argtypes = [C.POINTER(_GatedLayer), _i]
+_lib.hire_gated_ffn_step.restype = _i
+_lib.hire_gated_ffn_step.argtypes = [C.POINTER(_GatedLayer), _vp, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.hire_gated_ffn_backward.restype = _i
+_lib.hire_gated_ffn_backward.argtypes = [C.POINTER(_GatedLayer), _vp, _i] + [_vp] * 9 + [_sz, _vp]
+
+
 class HireError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -498,6 +513,85 @@ def topk_select(scores: torch.Tensor, k: int, relu: bool = False, rank_order: bo
     _check(_lib.topk_select(_ptr(scores), B, N, k, flags, _ptr(idx), _ptr(val), _ptr(ws), ws.numel(), _stream(stream)),
            "topk_select")
     return idx, val
+
+
+def _tensor(t, dtype, shape, where):
+    """The address of a contiguous tensor of this type and shape on the current device."""
+    if (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda or
+            t.get_device() != _current_device()):
+        raise HireError(EINVAL, f"{where}: contiguous {dtype} {tuple(shape)} on the current device wanted, got {t.dtype} "
+                                f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2
+_ACTS = {"relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU}
+
+
+class GatedLayer:
+    """A dense gated FFN layer: bf16 [d_ff, d_model] device matrices wg (the gate), wu and w2u, unit-major."""
+
+    def __init__(self, wg, wu, w2u, act="silu"):
+        for t in (wg, wu, w2u):
+            if t.dim() != 2 or t.shape != wg.shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or not t.is_cuda:
+                raise HireError(EINVAL, "GatedLayer: contiguous bf16 [d_ff, d_model] device matrices")
+        if act not in _ACTS:
+            raise HireError(EINVAL, f"GatedLayer: act is one of {sorted(_ACTS)}")
+        self.wg, self.wu, self.w2u, self.act = wg, wu, w2u, act
+        self.d_ff, self.d_model = wg.shape
+        self.c = _GatedLayer(self.d_model, self.d_ff, wg.data_ptr(), wu.data_ptr(), w2u.data_ptr(), _ACTS[act])
+        self.ref = C.byref(self.c)
+
+
+class GatedOutputs:
+    """Caller-owned output of hire_gated_ffn_step; train=True: with what the backward call reads."""
+
+    def __init__(self, layer: GatedLayer, T: int, train: bool = False):
+        dev = layer.wg.device
+        self.y = torch.empty((T, layer.d_model), dtype=torch.bfloat16, device=dev)
+        self.g, self.u, self.h = (torch.empty((T, layer.d_ff), dtype=torch.bfloat16, device=dev) if train else None
+                                  for _ in range(3))
+
+
+class GatedGradients:
+    """Caller-owned outputs of hire_gated_ffn_backward: dx [T, d_model], dwg, dwu, dw2u [d_ff, d_model], bf16.  Set one to
+    None to leave it out."""
+
+    def __init__(self, layer: GatedLayer, T: int):
+        self.dx = torch.empty((T, layer.d_model), dtype=torch.bfloat16, device=layer.wg.device)
+        self.dwg, self.dwu, self.dw2u = (torch.empty_like(layer.wg) for _ in range(3))
+
+
+def hire_gated_ffn_workspace_bytes(layer: GatedLayer, T: int) -> int:
+    return int(_lib.hire_gated_ffn_workspace_bytes(layer.ref, T))
+
+
+def hire_gated_ffn_backward_workspace_bytes(layer: GatedLayer, T: int) -> int:
+    return int(_lib.hire_gated_ffn_backward_workspace_bytes(layer.ref, T))
+
+
+def hire_gated_ffn_step(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, workspace: torch.Tensor,
+                        stream=None) -> None:
+    """Enqueue the dense gated FFN of x bf16 [T, d_model]."""
+    where, bf16, T = "hire_gated_ffn_step", torch.bfloat16, x.shape[0]
+    tokens, hidden = (T, layer.d_model), (T, layer.d_ff)
+    kept = [None if t is None else _tensor(t, bf16, hidden, where) for t in (out.g, out.u, out.h)]
+    _check(_lib.hire_gated_ffn_step(layer.ref, _tensor(x, bf16, tokens, where), T, _tensor(out.y, bf16, tokens, where), *kept,
+                                    _ptr(workspace), workspace.numel(), _stream(stream)), where)
+
+
+def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, dy: torch.Tensor,
+                            grads: GatedGradients, workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue the gradients for dy bf16 [T, d_model]; `out` as the forward call with train=True left it."""
+    where, bf16, T = "hire_gated_ffn_backward", torch.bfloat16, x.shape[0]
+    tokens, hidden, weights = (T, layer.d_model), (T, layer.d_ff), (layer.d_ff, layer.d_model)
+    if out.g is None:
+        raise HireError(EINVAL, f"{where}: outputs made with train=True")
+    kept = [_tensor(t, bf16, hidden, where) for t in (out.g, out.u, out.h)]
+    wanted = [None if t is None else _tensor(t, bf16, shape, where)
+              for t, shape in ((grads.dx, tokens), (grads.dwg, weights), (grads.dwu, weights), (grads.dw2u, weights))]
+    _check(_lib.hire_gated_ffn_backward(layer.ref, _tensor(x, bf16, tokens, where), T, *kept, _tensor(dy, bf16, tokens, where),
+                                        *wanted, _ptr(workspace), workspace.numel(), _stream(stream)), where)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:
