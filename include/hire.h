@@ -302,6 +302,40 @@ int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, con
                             const void* dy, void* dx, void* dwg, void* dwu, void* dw2u, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- Microscaled 4-bit floating point (MXFP4) ------------------------------------------------------------------------
+ * Blocks of 32 neighbouring values of a row: each a 4-bit code (sign, two bits of exponent, one of significand: 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives) times the block's power of two 2^(byte - 127).  codes: [rows, cols / 2] bytes, the
+ * value of the lower column in the low nibble; scales: [rows, cols / 32] bytes.  Both are rows in order without gaps,
+ * codes 16-byte aligned; cols is a multiple of 32. */
+#define HIRE_F32 0
+#define HIRE_BF16 1
+
+#define HIRE_MXFP4_MAX_TOKENS (1 << 20)
+#define HIRE_MXFP4_MAX_ROWS (1 << 24)
+#define HIRE_MXFP4_MAX_COLS (1 << 20)
+
+/* w_bf16 [rows, cols], 16-byte aligned -> codes and scales.  A block's power of two is 2^(floor(log2 amax) - 2), at least
+ * 2^-127; values are rounded to the nearest code, half steps to the even one, and magnitudes beyond 6 (up to 8 in these
+ * units) become 6.  A block of zeros has the byte 127; a block that holds an infinity or a NaN has the byte 255 (not a
+ * number) and codes of 0. */
+int hire_pack_mxfp4(const void* w_bf16, int rows, int cols, void* codes, void* scales, void* stream);
+
+/* The values that codes and scales stand for, in bf16: exact, but that magnitudes beyond bf16's largest (scale bytes above
+ * 252, which hire_pack_mxfp4 never writes, 255 apart) become infinite; NaN for blocks of byte 255. */
+int hire_unpack_mxfp4(const void* codes, const void* scales, int rows, int cols, void* w_bf16, void* stream);
+
+/* y[t, j] = sum_i x[t, i] w[j, i], w [rows, cols] packed; fp32 sums.  y: [T, rows], 16-byte aligned, of y_type HIRE_F32 or
+ * HIRE_BF16 (rounded once).  hire_mxfp4_product: x packed too, 1 <= T <= HIRE_MXFP4_MAX_TOKENS; products and scales are
+ * exact.  hire_mxfp4_product_bf16: x bf16 [T, cols], 16-byte aligned, 1 <= T <= HIRE_MAX_BATCH (more: HIRE_EUNSUPPORTED);
+ * the weights are those of hire_unpack_mxfp4.  A NaN block makes its row's results NaN.  workspace:
+ * hire_mxfp4_product_workspace_bytes(T, rows, cols) bytes (0 on invalid arguments), 256-byte aligned; no initialisation
+ * needed, and hire_workspace_init does no harm. */
+size_t hire_mxfp4_product_workspace_bytes(int T, int rows, int cols);
+int hire_mxfp4_product(const void* x_codes, const void* x_scales, int T, const void* w_codes, const void* w_scales, int rows,
+                       int cols, void* y, int y_type, void* workspace, size_t workspace_bytes, void* stream);
+int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const void* w_scales, int rows, int cols, void* y,
+                            int y_type, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

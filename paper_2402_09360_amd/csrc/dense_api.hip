@@ -35,6 +35,22 @@ GatedLayer gated_layer(const hire_gated_layer* L) {
 }
 uint16_t* bf16_at(void* base, size_t off) { return reinterpret_cast<uint16_t*>(static_cast<char*>(base) + off); }
 
+int check_mx(int T, int rows, int cols) {
+  if (T < 1 || rows < 1 || cols < 32 || cols % 32 != 0) return HIRE_EINVAL;
+  if (T > HIRE_MXFP4_MAX_TOKENS || rows > HIRE_MXFP4_MAX_ROWS || cols > HIRE_MXFP4_MAX_COLS) return HIRE_EUNSUPPORTED;
+  return HIRE_OK;
+}
+int mx_product(const void* x, const uint8_t* x_scales, int T, const void* w_codes, const void* w_scales, int rows, int cols,
+               void* y, int y_type, void* workspace, size_t workspace_bytes, void* stream) {
+  if (const int rc = check_mx(T, rows, cols); rc != HIRE_OK) return rc;
+  if (!given(w_codes, 16) || !w_scales || !given(y, 16) || !given(workspace, 256)) return HIRE_EINVAL;
+  if (y_type != HIRE_F32 && y_type != HIRE_BF16) return HIRE_EINVAL;
+  if (workspace_bytes < hire_mxfp4_product_workspace_bytes(T, rows, cols)) return HIRE_ENOSPC;
+  return launched(launch_mx_product(MxProduct{x, x_scales, T, static_cast<const uint8_t*>(w_codes),
+                                              static_cast<const uint8_t*>(w_scales), rows, cols, y, y_type == HIRE_BF16},
+                                    static_cast<hipStream_t>(stream)));
+}
+
 size_t hidden_bytes(const hire_gated_layer* L, int T) { return align_up((size_t)T * L->d_ff * 2); }
 
 }  // namespace
@@ -81,6 +97,38 @@ int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, con
       static_cast<uint16_t*>(dwg), static_cast<uint16_t*>(dwu), static_cast<uint16_t*>(dw2u), bf16_at(workspace, 0),
       bf16_at(workspace, hidden), reinterpret_cast<float*>(bf16_at(workspace, 2 * hidden)),
       static_cast<hipStream_t>(stream)));
+}
+
+int hire_pack_mxfp4(const void* w_bf16, int rows, int cols, void* codes, void* scales, void* stream) {
+  if (rows < 1 || cols < 32 || cols % 32 != 0 || !given(w_bf16, 16) || !given(codes, 16) || !scales) return HIRE_EINVAL;
+  return launched(launch_pack_mxfp4(static_cast<const uint16_t*>(w_bf16), rows, cols, static_cast<uint8_t*>(codes),
+                                    static_cast<uint8_t*>(scales), static_cast<hipStream_t>(stream)));
+}
+
+int hire_unpack_mxfp4(const void* codes, const void* scales, int rows, int cols, void* w_bf16, void* stream) {
+  if (rows < 1 || cols < 32 || cols % 32 != 0 || !given(w_bf16, 16) || !given(codes, 16) || !scales) return HIRE_EINVAL;
+  return launched(launch_unpack_mxfp4(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), rows, cols,
+                                      static_cast<uint16_t*>(w_bf16), static_cast<hipStream_t>(stream)));
+}
+
+size_t hire_mxfp4_product_workspace_bytes(int T, int rows, int cols) {
+  if (check_mx(T, rows, cols) != HIRE_OK) return 0;
+  return kAlign;
+}
+
+int hire_mxfp4_product(const void* x_codes, const void* x_scales, int T, const void* w_codes, const void* w_scales, int rows,
+                       int cols, void* y, int y_type, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!given(x_codes, 16) || !x_scales) return HIRE_EINVAL;
+  return mx_product(x_codes, static_cast<const uint8_t*>(x_scales), T, w_codes, w_scales, rows, cols, y, y_type, workspace,
+                    workspace_bytes, stream);
+}
+
+int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const void* w_scales, int rows, int cols, void* y,
+                            int y_type, void* workspace, size_t workspace_bytes, void* stream) {
+  static_assert(HIRE_MAX_BATCH == kMxFewTokens, "the tokens of a decode step");
+  if (!given(x, 16)) return HIRE_EINVAL;
+  if (T > HIRE_MAX_BATCH) return HIRE_EUNSUPPORTED;
+  return mx_product(x, nullptr, T, w_codes, w_scales, rows, cols, y, y_type, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -489,6 +489,22 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
                                  const uint16_t* h, const uint16_t* dy, uint16_t* dx, uint16_t* dwg, uint16_t* dwu,
                                  uint16_t* dw2u, uint16_t* dg, uint16_t* du, float* part, hipStream_t s);
 
+// ---- mxfp4.hip: microscaled 4-bit floating point ---------------------------------
+hipError_t launch_pack_mxfp4(const uint16_t* w, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s);
+hipError_t launch_unpack_mxfp4(const uint8_t* codes, const uint8_t* scales, int rows, int cols, uint16_t* w, hipStream_t s);
+constexpr int kMxFewTokens = 64;  // bf16 tokens: the most
+struct MxProduct {
+  const void* x;            // bf16 [T, cols], or codes [T, cols / 2] with x_scales
+  const uint8_t* x_scales;  // [T, cols / 32], or null: bf16 tokens
+  int T;
+  const uint8_t* codes;     // [rows, cols / 2]
+  const uint8_t* scales;    // [rows, cols / 32]
+  int rows, cols;
+  void* y;                  // [T, rows], bf16 or fp32
+  int y_bf16;
+};
+hipError_t launch_mx_product(const MxProduct& p, hipStream_t s);
+
 // The HIP error behind the calling thread's most recent HIRE_ELAUNCH (api.hip).
 hipError_t& last_launch_error();
 

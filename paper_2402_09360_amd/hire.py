@@ -131,6 +131,15 @@ _lib.hire_gated_ffn_step.argtypes = [C.POINTER(_GatedLayer), _vp, _i, _vp, _vp, 
 _lib.hire_gated_ffn_backward.restype = _i
 _lib.hire_gated_ffn_backward.argtypes = [C.POINTER(_GatedLayer), _vp, _i] + [_vp] * 9 + [_sz, _vp]
 
+_lib.hire_pack_mxfp4.restype = _lib.hire_unpack_mxfp4.restype = _i
+_lib.hire_pack_mxfp4.argtypes = [_vp, _i, _i, _vp, _vp, _vp]
+_lib.hire_unpack_mxfp4.argtypes = [_vp, _vp, _i, _i, _vp, _vp]
+_lib.hire_mxfp4_product_workspace_bytes.restype = _sz
+_lib.hire_mxfp4_product_workspace_bytes.argtypes = [_i, _i, _i]
+_lib.hire_mxfp4_product.restype = _lib.hire_mxfp4_product_bf16.restype = _i
+_lib.hire_mxfp4_product.argtypes = [_vp, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _vp, _sz, _vp]
+_lib.hire_mxfp4_product_bf16.argtypes = [_vp, _i, _vp, _vp, _i, _i, _vp, _i, _vp, _sz, _vp]
+
 
 class HireError(RuntimeError):
     def __init__(self, code: int, where: str):
@@ -592,6 +601,86 @@ def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutput
               for t, shape in ((grads.dx, tokens), (grads.dwg, weights), (grads.dwu, weights), (grads.dw2u, weights))]
     _check(_lib.hire_gated_ffn_backward(layer.ref, _tensor(x, bf16, tokens, where), T, *kept, _tensor(dy, bf16, tokens, where),
                                         *wanted, _ptr(workspace), workspace.numel(), _stream(stream)), where)
+
+
+F32, BF16 = 0, 1
+
+
+class Mxfp4:
+    """A matrix [rows, cols] in microscaled 4-bit floating point: uint8 device tensors codes [rows, cols / 2] (the lower
+    column in the low nibble) and scales [rows, cols / 32] (a power of two 2^(byte - 127) for 32 columns)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        for t in (codes, scales):
+            if t.dtype != torch.uint8 or t.dim() != 2 or not t.is_contiguous() or not t.is_cuda:
+                raise HireError(EINVAL, "Mxfp4: contiguous two-dimensional uint8 device tensors")
+        if codes.shape != (scales.shape[0], 16 * scales.shape[1]) or codes.device != scales.device:
+            raise HireError(EINVAL, "Mxfp4: codes [rows, cols / 2] and scales [rows, cols / 32] of one matrix")
+        self.codes, self.scales = codes, scales
+        self.rows, self.cols = codes.shape[0], 2 * codes.shape[1]
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, device="cuda"):
+        if rows < 1 or cols < 32 or cols % 32:
+            raise HireError(EINVAL, "Mxfp4: cols is a multiple of 32")
+        return cls(torch.empty((rows, cols // 2), dtype=torch.uint8, device=device),
+                   torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
+
+    def _addresses(self, where):
+        if self.codes.get_device() != _current_device():
+            raise HireError(EINVAL, f"{where}: packed matrix on the current device wanted, got {self.codes.device}")
+        return self.codes.data_ptr(), self.scales.data_ptr()
+
+
+def hire_pack_mxfp4(w: torch.Tensor, out: Mxfp4 | None = None, stream=None) -> Mxfp4:
+    """w bf16 [rows, cols] in microscaled 4-bit floating point; out: where to write it."""
+    where = "hire_pack_mxfp4"
+    if w.dim() != 2:
+        raise HireError(EINVAL, f"{where}: a matrix")
+    if out is None:
+        out = Mxfp4.empty(w.shape[0], w.shape[1], w.device)
+    at = _tensor(w, torch.bfloat16, (out.rows, out.cols), where)
+    _check(_lib.hire_pack_mxfp4(at, out.rows, out.cols, *out._addresses(where), _stream(stream)), where)
+    return out
+
+
+def hire_unpack_mxfp4(w: Mxfp4, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The values a packed matrix stands for, bf16 [rows, cols]."""
+    where = "hire_unpack_mxfp4"
+    if out is None:
+        out = torch.empty((w.rows, w.cols), dtype=torch.bfloat16, device=w.codes.device)
+    at = _tensor(out, torch.bfloat16, (w.rows, w.cols), where)
+    _check(_lib.hire_unpack_mxfp4(*w._addresses(where), w.rows, w.cols, at, _stream(stream)), where)
+    return out
+
+
+def hire_mxfp4_product_workspace_bytes(T: int, rows: int, cols: int) -> int:
+    return int(_lib.hire_mxfp4_product_workspace_bytes(T, rows, cols))
+
+
+def _product_output(y, T, rows, where):
+    y_type = {torch.float32: F32, torch.bfloat16: BF16}.get(y.dtype)
+    if y_type is None:
+        raise HireError(EINVAL, f"{where}: y is float32 or bfloat16")
+    return _tensor(y, y.dtype, (T, rows), where), y_type
+
+
+def hire_mxfp4_product(x: Mxfp4, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue y [T, rows] (float32 or bfloat16) = x w^T, both packed."""
+    where = "hire_mxfp4_product"
+    if x.cols != w.cols:
+        raise HireError(EINVAL, f"{where}: {x.cols} and {w.cols} columns")
+    _check(_lib.hire_mxfp4_product(*x._addresses(where), x.rows, *w._addresses(where), w.rows, w.cols,
+                                   *_product_output(y, x.rows, w.rows, where), _ptr(workspace), workspace.numel(),
+                                   _stream(stream)), where)
+
+
+def hire_mxfp4_product_bf16(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue y [T, rows] (float32 or bfloat16) = x w^T for x bf16 [T, cols], at most MAX_BATCH tokens."""
+    where, T = "hire_mxfp4_product_bf16", x.shape[0]
+    _check(_lib.hire_mxfp4_product_bf16(_tensor(x, torch.bfloat16, (T, w.cols), where), T, *w._addresses(where), w.rows, w.cols,
+                                        *_product_output(y, T, w.rows, where), _ptr(workspace), workspace.numel(),
+                                        _stream(stream)), where)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

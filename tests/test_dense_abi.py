@@ -55,3 +55,35 @@ def test_gated_refusals(hire):
     assert back(outs=(None,) * 4) == EINVAL and back(outs=(0x1008, None, None, None)) == EINVAL
     assert back(outs=(None, None, None, 0x1000)) == ENOSPC
     assert hire._lib.hire_gated_ffn_step(None, 0x40000, 1, 0x50000, None, None, None, 0x60000, 256, None) == EINVAL
+
+
+def test_mxfp4_refusals(hire):
+    lib = hire._lib
+    for f in (lambda rows, cols, w=0x1000, c=0x2000, s=0x3001: lib.hire_pack_mxfp4(w, rows, cols, c, s, None),
+              lambda rows, cols, w=0x1000, c=0x2000, s=0x3001: lib.hire_unpack_mxfp4(c, s, rows, cols, w, None)):
+        for rows, cols in ((0, 32), (-1, 32), (1, 0), (1, 16), (1, 40), (1, -32)):
+            assert f(rows, cols) == EINVAL
+        assert f(1, 32, w=None) == EINVAL and f(1, 32, c=None) == EINVAL and f(1, 32, s=None) == EINVAL
+        assert f(1, 32, w=0x1008) == EINVAL and f(1, 32, c=0x2004) == EINVAL
+
+    size = lib.hire_mxfp4_product_workspace_bytes
+    assert size(1, 1, 32) > 0 and size(1 << 20, 1 << 24, 1 << 20) > 0
+    limits = [((0, 5, 64), EINVAL), ((1, 0, 64), EINVAL), ((1, 5, 0), EINVAL), ((1, 5, 48), EINVAL),
+              (((1 << 20) + 1, 5, 64), EUNSUPPORTED), ((1, (1 << 24) + 1, 64), EUNSUPPORTED), ((1, 5, (1 << 20) + 32), EUNSUPPORTED)]
+
+    def packed(T=2, rows=5, cols=64, x=0x1000, xs=0x2000, w=0x3000, s=0x4000, y=0x5000, kind=0, ws=0x6000, nbytes=0):
+        return lib.hire_mxfp4_product(x, xs, T, w, s, rows, cols, y, kind, ws, nbytes, None)
+
+    def bf16(T=2, rows=5, cols=64, x=0x1000, w=0x3000, s=0x4000, y=0x5000, kind=0, ws=0x6000, nbytes=0):
+        return lib.hire_mxfp4_product_bf16(x, T, w, s, rows, cols, y, kind, ws, nbytes, None)
+
+    for call in (packed, bf16):
+        assert call() == ENOSPC and call(kind=1) == ENOSPC
+        assert call(kind=2) == EINVAL and call(kind=-1) == EINVAL
+        for (T, rows, cols), code in limits:
+            assert call(T=T, rows=rows, cols=cols) == code and size(T, rows, cols) == 0
+        for name in ("x", "w", "y", "ws"):
+            assert call(**{name: None}) == EINVAL and call(**{name: 0x1008}) == EINVAL
+        assert call(s=None) == EINVAL
+    assert packed(xs=None) == EINVAL
+    assert bf16(T=65) == EUNSUPPORTED and packed(T=65) == ENOSPC
