@@ -10,8 +10,8 @@
  *
  * General rules, valid for every entry point below:
  *   - Every pointer is a DEVICE pointer owned by the caller unless it is one
- *     of the two layer descriptor structs, which are HOST structs holding
- *     device pointers.  The library allocates nothing and frees nothing.
+ *     of the descriptor structs (the layers, hire_drafts), which are HOST
+ *     structs holding device pointers.  The library allocates nothing and frees nothing.
  *   - Work is enqueued on `stream` (a hipStream_t passed as void*; NULL is
  *     the default stream).  No entry point synchronises.
  *   - All matrices are row-major and "unit-major": row j is the vector of
@@ -335,6 +335,45 @@ int hire_mxfp4_product(const void* x_codes, const void* x_scales, int T, const v
                        int cols, void* y, int y_type, void* workspace, size_t workspace_bytes, void* stream);
 int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const void* w_scales, int rows, int cols, void* y,
                             int y_type, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Verification of drafted tokens ----------------------------------------------------------------------------------
+ * B sequences, each with up to n tokens that a draft proposed, and the target's distributions at their positions and behind
+ * the last one.  Token i of a sequence is accepted iff all in front of it are and
+ *   u_i q_i(d_i) < p_i(d_i)
+ * (u_i from [0, 1), q the draft's distribution, p the target's).  Behind the a accepted ones one more token follows: with
+ * r(v) = max(p_a(v) - q_a(v), 0) if token a was refused, r = p_a if none was left (or if no r(v) is positive), it is
+ * the first v with  sum_{w <= v} r(w) > s sum_w r(w),  s from [0, 1); -1 if p_a has no positive value.  Differences
+ * and sums are fp64.
+ * A distribution is a dense row of `vocab` probabilities, where "first" counts tokens, or a list of k (token, probability)
+ * pairs as hire_softmax_step leaves it, 0 elsewhere, where "first" counts places in the target's list.  Of entries that
+ * name one token the first counts; entries whose token is not in [0, vocab) do not.  A drafted token outside [0, vocab)
+ * is refused, and taken off nothing.  Probabilities need not add up to 1. */
+#define HIRE_MAX_DRAFT 63
+#define HIRE_MAX_DRAFT_BATCH 4096
+#define HIRE_MAX_DRAFT_VOCAB (1 << 22)
+
+typedef struct hire_drafts {
+  int B;                      /* sequences, 1 .. HIRE_MAX_DRAFT_BATCH */
+  int n;                      /* most drafted tokens of a sequence, 0 .. HIRE_MAX_DRAFT */
+  int vocab;                  /* 1 .. HIRE_MAX_DRAFT_VOCAB */
+  const int32_t* lengths;     /* optional [B]: drafted tokens of each sequence (clamped to 0 .. n); NULL: n */
+  const int32_t* tokens;      /* [B, n]; places behind a sequence's length are not read */
+  const float* target_prob;   /* fp32 [B, n + 1, vocab], or [B, n + 1, target_k] */
+  const int32_t* target_idx;  /* lists: int32 [B, n + 1, target_k]; NULL: dense */
+  int target_k;               /* 1 .. HIRE_MAX_RANK_ORDER_K, lists only */
+  const float* draft_prob;    /* fp32 [B, n, vocab] or [B, n, draft_k]; NULL: every drafted token was certain (q = 1) */
+  const int32_t* draft_idx;   /* lists: int32 [B, n, draft_k]; NULL: dense */
+  int draft_k;                /* 1 .. HIRE_MAX_RANK_ORDER_K, lists only */
+  const float* accept_u;      /* fp32 [B, n] */
+  const float* sample_u;      /* fp32 [B] */
+} hire_drafts;                /* HOST struct; with n = 0 tokens and accept_u may be NULL and draft_prob must be */
+
+/* tokens_out int32 [B, n + 1]: the accepted tokens, the one that follows, then -1; accepted_out int32 [B].  workspace:
+ * hire_verify_draft_workspace_bytes(D) bytes (0 on invalid arguments), 256-byte aligned; no initialisation needed, and
+ * hire_workspace_init does no harm.  Beyond a limit: HIRE_EUNSUPPORTED. */
+size_t hire_verify_draft_workspace_bytes(const hire_drafts* D);
+int hire_verify_draft(const hire_drafts* D, int32_t* tokens_out, int32_t* accepted_out, void* workspace,
+                      size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

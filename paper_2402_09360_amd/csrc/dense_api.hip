@@ -51,6 +51,20 @@ int mx_product(const void* x, const uint8_t* x_scales, int T, const void* w_code
                                     static_cast<hipStream_t>(stream)));
 }
 
+int check_drafts(const hire_drafts* D) {
+  static_assert(HIRE_MAX_DRAFT == kMaxDraft && HIRE_MAX_RANK_ORDER_K == kMaxDraftList, "same numbers");
+  if (!D || D->B < 1 || D->n < 0 || D->vocab < 1) return HIRE_EINVAL;
+  if (!given(D->target_prob, 4) || !optional(D->target_idx, 4) || !optional(D->draft_prob, 4) || !optional(D->draft_idx, 4))
+    return HIRE_EINVAL;
+  if (!optional(D->lengths, 4) || !given(D->sample_u, 4) || (D->draft_idx && !D->draft_prob)) return HIRE_EINVAL;
+  if (D->n > 0 ? !given(D->tokens, 4) || !given(D->accept_u, 4) : D->draft_prob != nullptr) return HIRE_EINVAL;
+  if ((D->target_idx && D->target_k < 1) || (D->draft_idx && D->draft_k < 1)) return HIRE_EINVAL;
+  if (D->B > HIRE_MAX_DRAFT_BATCH || D->n > HIRE_MAX_DRAFT || D->vocab > HIRE_MAX_DRAFT_VOCAB) return HIRE_EUNSUPPORTED;
+  if ((D->target_idx && D->target_k > HIRE_MAX_RANK_ORDER_K) || (D->draft_idx && D->draft_k > HIRE_MAX_RANK_ORDER_K))
+    return HIRE_EUNSUPPORTED;
+  return HIRE_OK;
+}
+
 size_t hidden_bytes(const hire_gated_layer* L, int T) { return align_up((size_t)T * L->d_ff * 2); }
 
 }  // namespace
@@ -129,6 +143,28 @@ int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const voi
   if (!given(x, 16)) return HIRE_EINVAL;
   if (T > HIRE_MAX_BATCH) return HIRE_EUNSUPPORTED;
   return mx_product(x, nullptr, T, w_codes, w_scales, rows, cols, y, y_type, workspace, workspace_bytes, stream);
+}
+
+size_t hire_verify_draft_workspace_bytes(const hire_drafts* D) {
+  if (check_drafts(D) != HIRE_OK) return 0;
+  if (D->target_idx) return kAlign;
+  return align_up((size_t)D->B * draft_parts(D->B, D->vocab).count * 2 * sizeof(double));
+}
+
+int hire_verify_draft(const hire_drafts* D, int32_t* tokens_out, int32_t* accepted_out, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  if (const int rc = check_drafts(D); rc != HIRE_OK) return rc;
+  if (!given(tokens_out, 4) || !given(accepted_out, 4) || !given(workspace, 256)) return HIRE_EINVAL;
+  if (workspace_bytes < hire_verify_draft_workspace_bytes(D)) return HIRE_ENOSPC;
+  DraftArgs a{};
+  a.B = D->B, a.n = D->n, a.vocab = D->vocab;
+  a.lengths = D->lengths, a.tokens = D->tokens;
+  a.target = D->target_prob, a.target_idx = D->target_idx, a.target_k = D->target_k;
+  a.draft = D->draft_prob, a.draft_idx = D->draft_idx, a.draft_k = D->draft_k;
+  a.accept_u = D->accept_u, a.sample_u = D->sample_u;
+  a.out_tokens = tokens_out, a.accepted = accepted_out;
+  a.part = static_cast<double*>(workspace);
+  return launched(launch_verify(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

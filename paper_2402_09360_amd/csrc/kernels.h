@@ -505,6 +505,33 @@ struct MxProduct {
 };
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s);
 
+// ---- verify.hip: drafted tokens against the target's probabilities ----------------
+constexpr int kMaxDraft = 63;          // drafted tokens of a sequence: with the one behind them a wave's lanes
+constexpr int kMaxDraftList = 4096;    // entries of a list
+constexpr int kMaxDraftPart = 16384;   // tokens of a dense row that one workgroup sums
+struct DraftArgs {
+  int B, n, vocab;
+  const int32_t* lengths;     // [B] or null: all n
+  const int32_t* tokens;      // [B, n]
+  const float* target;        // [B, n + 1, vocab], or lists [B, n + 1, target_k] with
+  const int32_t* target_idx;
+  int target_k;
+  const float* draft;         // [B, n, vocab], or lists [B, n, draft_k] with draft_idx, or null: 1 for the drafted token
+  const int32_t* draft_idx;
+  int draft_k;
+  const float* accept_u;      // [B, n]
+  const float* sample_u;      // [B]
+  int32_t* out_tokens;        // [B, n + 1]
+  int32_t* accepted;          // [B]
+  double* part;               // dense target: sums of the parts, a pair each
+  int parts, part_size;       // set by launch_verify
+};
+struct DraftParts {
+  int count, size;
+};
+DraftParts draft_parts(int B, int vocab);  // dense target
+hipError_t launch_verify(DraftArgs a, hipStream_t s);
+
 // The HIP error behind the calling thread's most recent HIRE_ELAUNCH (api.hip).
 hipError_t& last_launch_error();
 

@@ -141,6 +141,19 @@ _lib.hire_mxfp4_product.argtypes = [_vp, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _vp
 _lib.hire_mxfp4_product_bf16.argtypes = [_vp, _i, _vp, _vp, _i, _i, _vp, _i, _vp, _sz, _vp]
 
 
+class _Drafts(C.Structure):
+    _fields_ = [("B", C.c_int), ("n", C.c_int), ("vocab", C.c_int), ("lengths", C.c_void_p), ("tokens", C.c_void_p),
+                ("target_prob", C.c_void_p), ("target_idx", C.c_void_p), ("target_k", C.c_int),
+                ("draft_prob", C.c_void_p), ("draft_idx", C.c_void_p), ("draft_k", C.c_int), ("accept_u", C.c_void_p),
+                ("sample_u", C.c_void_p)]
+
+
+_lib.hire_verify_draft_workspace_bytes.restype = _sz
+_lib.hire_verify_draft_workspace_bytes.argtypes = [C.POINTER(_Drafts)]
+_lib.hire_verify_draft.restype = _i
+_lib.hire_verify_draft.argtypes = [C.POINTER(_Drafts), _vp, _vp, _vp, _sz, _vp]
+
+
 class HireError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -681,6 +694,59 @@ def hire_mxfp4_product_bf16(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspac
     _check(_lib.hire_mxfp4_product_bf16(_tensor(x, torch.bfloat16, (T, w.cols), where), T, *w._addresses(where), w.rows, w.cols,
                                         *_product_output(y, T, w.rows, where), _ptr(workspace), workspace.numel(),
                                         _stream(stream)), where)
+
+
+class Drafts:
+    """Drafted tokens int32 [B, n] with the target's distributions [B, n + 1, ...] and the draft's [B, n, ...] (None: every
+    token was certain), fp32: dense rows of vocab probabilities, or lists with the int32 tokens of the same shape, as
+    hire_softmax_step leaves them.  accept_u fp32 [B, n] and sample_u fp32 [B] from [0, 1); lengths int32 [B]: how many tokens
+    of each row are drafts (all).  The tensors are kept; their contents may change from call to call."""
+
+    def __init__(self, tokens, vocab, target_prob, accept_u, sample_u, target_idx=None, draft_prob=None, draft_idx=None,
+                 lengths=None):
+        B, n = tokens.shape
+        where, i32, f32 = "Drafts", torch.int32, torch.float32
+        k = [None, None]
+
+        def rows(prob, idx, positions, which):
+            if prob is None:
+                if idx is not None:
+                    raise HireError(EINVAL, f"{where}: tokens of a list without probabilities")
+                return None, None
+            width = vocab
+            if idx is not None:
+                width = k[which] = idx.shape[2] if idx.dim() == 3 else 0
+            return (_tensor(prob, f32, (B, positions, width), where),
+                    None if idx is None else _tensor(idx, i32, (B, positions, width), where))
+
+        p, p_idx = rows(target_prob, target_idx, n + 1, 0)
+        q, q_idx = rows(draft_prob, draft_idx, n, 1)
+        self.B, self.n, self.vocab, self.device = B, n, vocab, tokens.device
+        self.tensors = (tokens, target_prob, target_idx, draft_prob, draft_idx, accept_u, sample_u, lengths)
+        self.c = _Drafts(B, n, vocab, None if lengths is None else _tensor(lengths, i32, (B,), where),
+                         _tensor(tokens, i32, (B, n), where) or None, p, p_idx, k[0] or 0, q, q_idx, k[1] or 0,
+                         _tensor(accept_u, f32, (B, n), where) or None, _tensor(sample_u, f32, (B,), where))
+        self.ref = C.byref(self.c)
+
+
+class DraftOutputs:
+    """Caller-owned outputs of hire_verify_draft: tokens int32 [B, n + 1], accepted int32 [B]."""
+
+    def __init__(self, drafts: Drafts):
+        self.tokens = torch.empty((drafts.B, drafts.n + 1), dtype=torch.int32, device=drafts.device)
+        self.accepted = torch.empty(drafts.B, dtype=torch.int32, device=drafts.device)
+
+
+def hire_verify_draft_workspace_bytes(drafts: Drafts) -> int:
+    return int(_lib.hire_verify_draft_workspace_bytes(drafts.ref))
+
+
+def hire_verify_draft(drafts: Drafts, out: DraftOutputs, workspace: torch.Tensor, stream=None) -> None:
+    """Enqueue the verification: the accepted tokens and the one that follows, and how many were accepted."""
+    where = "hire_verify_draft"
+    _check(_lib.hire_verify_draft(drafts.ref, _tensor(out.tokens, torch.int32, (drafts.B, drafts.n + 1), where),
+                                  _tensor(out.accepted, torch.int32, (drafts.B,), where), _ptr(workspace), workspace.numel(),
+                                  _stream(stream)), where)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

@@ -87,3 +87,33 @@ def test_mxfp4_refusals(hire):
         assert call(s=None) == EINVAL
     assert packed(xs=None) == EINVAL
     assert bf16(T=65) == EUNSUPPORTED and packed(T=65) == ENOSPC
+
+
+def test_draft_refusals(hire):
+    lib = hire._lib
+    base = dict(B=2, n=3, vocab=100, lengths=None, tokens=0x100, target_prob=0x200, target_idx=None, target_k=0,
+                draft_prob=0x300, draft_idx=None, draft_k=0, accept_u=0x400, sample_u=0x500)
+
+    def call(out=0x600, acc=0x700, ws=0x800, nbytes=0, **changes):
+        d = hire._Drafts(**{**base, **changes})
+        code = lib.hire_verify_draft(C.byref(d), out, acc, ws, nbytes, None)
+        size = lib.hire_verify_draft_workspace_bytes(C.byref(d))
+        return code, size
+
+    code, size = call()
+    assert code == ENOSPC and size > 0
+    lists = dict(target_idx=0x900, target_k=64, draft_idx=0xA00, draft_k=4096)
+    assert call(**lists)[0] == ENOSPC and call(lengths=0x40)[0] == ENOSPC and call(draft_prob=None)[0] == ENOSPC
+    assert call(n=0, tokens=None, accept_u=None, draft_prob=None)[0] == ENOSPC
+    for bad in (dict(B=0), dict(B=-1), dict(n=-1), dict(vocab=0), dict(tokens=None), dict(tokens=0x101), dict(target_prob=None),
+                dict(target_prob=0x202), dict(accept_u=None), dict(sample_u=None), dict(lengths=0x41), dict(n=0),
+                dict(draft_idx=0x900, draft_k=5, draft_prob=None), dict(target_idx=0x900, target_k=0),
+                dict(draft_idx=0x900, draft_k=0), dict(draft_idx=0x900, draft_k=-3), dict(target_idx=0x901, target_k=4)):
+        assert call(**bad) == (EINVAL, 0), bad
+    for bad in (dict(B=4097), dict(n=64), dict(vocab=(1 << 22) + 1), dict(target_idx=0x900, target_k=4097),
+                dict(draft_idx=0x900, draft_k=4097)):
+        assert call(**bad) == (EUNSUPPORTED, 0), bad
+    for bad in (dict(out=None), dict(acc=None), dict(ws=None), dict(out=0x602), dict(ws=0x810)):
+        assert call(**bad)[0] == EINVAL, bad
+    assert lib.hire_verify_draft(None, 0x600, 0x700, 0x800, 1 << 20, None) == EINVAL
+    assert call(B=4096, vocab=1 << 22)[1] > 0
