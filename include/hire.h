@@ -282,15 +282,17 @@ typedef struct hire_gated_layer {
 } hire_gated_layer;
 
 /* x, y: bf16 [T, d_model], 1 <= T <= HIRE_GATED_MAX_TOKENS; y is rounded once from fp32 sums over h, and h is rounded
- * to bf16 between the two layers.  g, u, h: bf16 [T, d_ff] each, 16-byte aligned: what hire_gated_ffn_backward reads; all
- * three, or all NULL where no backward pass follows.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on
- * invalid arguments, never 0 on valid ones), 256-byte aligned; no initialisation needed, and hire_workspace_init does no
- * harm.  x and y must not overlap.  HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
+ * to bf16 between the two layers.  saved: hire_gated_ffn_saved_bytes(L, T) bytes, 256-byte aligned, that receive what
+ * hire_gated_ffn_backward reads (opaque: h in bf16, g and u in 24 bits), or NULL where no backward pass follows; y does not
+ * depend on it.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on invalid arguments, never 0 on valid ones),
+ * 256-byte aligned; no initialisation needed, and hire_workspace_init does no harm.  x and y must not overlap.
+ * HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
 size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T);
-int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* g, void* u, void* h,
-                        void* workspace, size_t workspace_bytes, void* stream);
+size_t hire_gated_ffn_saved_bytes(const hire_gated_layer* L, int T);
+int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* saved, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
-/* Gradients of sum(dy * y), dy bf16 [T, d_model], from what the forward call left in g, u and h:
+/* Gradients of sum(dy * y), dy bf16 [T, d_model], from what the forward call left in saved, which stays as it is:
  *   dh = <v_j, dy_b>;  dg = dh u a'(g);  du = dh a(g)   (a'(0) = 0 for HIRE_ACT_RELU)
  *   dw2u_j = sum_b h_bj dy_b;  dwg_j = sum_b dg_bj x_b;  dwu_j = sum_b du_bj x_b;  dx_b = sum_j dg_bj wg_j + du_bj wu_j
  * dx bf16 [T, d_model]; dwg, dwu, dw2u bf16 [d_ff, d_model]: each is written whole (nothing is added to what was there),
@@ -298,9 +300,8 @@ int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y
  * Results are the same from call to call.  Alignment, workspace (hire_gated_ffn_backward_workspace_bytes) and errors as
  * for the forward call. */
 size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T);
-int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* g, const void* u, const void* h,
-                            const void* dy, void* dx, void* dwg, void* dwu, void* dw2u, void* workspace,
-                            size_t workspace_bytes, void* stream);
+int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* saved, const void* dy, void* dx,
+                            void* dwg, void* dwu, void* dw2u, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Microscaled 4-bit floating point (MXFP4) ------------------------------------------------------------------------
  * Blocks of 32 neighbouring values of a row: each a 4-bit code (sign, two bits of exponent, one of significand: 0, 0.5, 1,

@@ -66,6 +66,10 @@ int check_drafts(const hire_drafts* D) {
 }
 
 size_t hidden_bytes(const hire_gated_layer* L, int T) { return align_up((size_t)T * L->d_ff * 2); }
+GatedKept kept_planes(const hire_gated_layer* L, int T, void* saved) {
+  const size_t plane = hidden_bytes(L, T);
+  return GatedKept{bf16_at(saved, 0), bf16_at(saved, plane), bf16_at(saved, 2 * plane), bf16_at(saved, 3 * plane)};
+}
 
 }  // namespace
 
@@ -76,16 +80,19 @@ size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T) {
   return hidden_bytes(L, T) + align_up(gated_part_bytes(T, L->d_model, L->d_ff, 1));
 }
 
-int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* g, void* u, void* h,
-                        void* workspace, size_t workspace_bytes, void* stream) {
+size_t hire_gated_ffn_saved_bytes(const hire_gated_layer* L, int T) {
+  return check_gated(L, T) != HIRE_OK ? 0 : 4 * hidden_bytes(L, T);
+}
+
+int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* saved, void* workspace,
+                        size_t workspace_bytes, void* stream) {
   if (const int rc = check_gated(L, T); rc != HIRE_OK) return rc;
-  if (!gated_weights(L) || !given(x, 16) || !given(y, 16) || !given(workspace, 256)) return HIRE_EINVAL;
-  if (!optional(g, 16) || !optional(u, 16) || !optional(h, 16) || (!g != !u) || (!g != !h)) return HIRE_EINVAL;
+  if (!gated_weights(L) || !given(x, 16) || !given(y, 16) || !optional(saved, 256) || !given(workspace, 256))
+    return HIRE_EINVAL;
   if (workspace_bytes < hire_gated_ffn_workspace_bytes(L, T)) return HIRE_ENOSPC;
-  uint16_t* hidden = h ? static_cast<uint16_t*>(h) : bf16_at(workspace, 0);
+  const GatedKept kept = saved ? kept_planes(L, T, saved) : GatedKept{bf16_at(workspace, 0), nullptr, nullptr, nullptr};
   float* part = reinterpret_cast<float*>(bf16_at(workspace, hidden_bytes(L, T)));
-  return launched(launch_gated_forward(gated_layer(L), static_cast<const uint16_t*>(x), T, static_cast<uint16_t*>(y), hidden,
-                                       static_cast<uint16_t*>(g), static_cast<uint16_t*>(u), part,
+  return launched(launch_gated_forward(gated_layer(L), static_cast<const uint16_t*>(x), T, static_cast<uint16_t*>(y), kept, part,
                                        static_cast<hipStream_t>(stream)));
 }
 
@@ -94,23 +101,19 @@ size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T)
   return 2 * hidden_bytes(L, T) + align_up(gated_part_bytes(T, L->d_model, L->d_ff, 2));
 }
 
-int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* g, const void* u, const void* h,
-                            const void* dy, void* dx, void* dwg, void* dwu, void* dw2u, void* workspace,
-                            size_t workspace_bytes, void* stream) {
+int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* saved, const void* dy, void* dx,
+                            void* dwg, void* dwu, void* dw2u, void* workspace, size_t workspace_bytes, void* stream) {
   if (const int rc = check_gated(L, T); rc != HIRE_OK) return rc;
-  if (!gated_weights(L) || !given(x, 16) || !given(g, 16) || !given(u, 16) || !given(h, 16) || !given(dy, 16) ||
-      !given(workspace, 256))
-    return HIRE_EINVAL;
+  if (!gated_weights(L) || !given(x, 16) || !given(saved, 256) || !given(dy, 16) || !given(workspace, 256)) return HIRE_EINVAL;
   if (!optional(dx, 16) || !optional(dwg, 16) || !optional(dwu, 16) || !optional(dw2u, 16) || !(dx || dwg || dwu || dw2u))
     return HIRE_EINVAL;
   if (workspace_bytes < hire_gated_ffn_backward_workspace_bytes(L, T)) return HIRE_ENOSPC;
   const size_t hidden = hidden_bytes(L, T);
   return launched(launch_gated_backward(
-      gated_layer(L), static_cast<const uint16_t*>(x), T, static_cast<const uint16_t*>(g), static_cast<const uint16_t*>(u),
-      static_cast<const uint16_t*>(h), static_cast<const uint16_t*>(dy), static_cast<uint16_t*>(dx),
-      static_cast<uint16_t*>(dwg), static_cast<uint16_t*>(dwu), static_cast<uint16_t*>(dw2u), bf16_at(workspace, 0),
-      bf16_at(workspace, hidden), reinterpret_cast<float*>(bf16_at(workspace, 2 * hidden)),
-      static_cast<hipStream_t>(stream)));
+      gated_layer(L), static_cast<const uint16_t*>(x), T, kept_planes(L, T, const_cast<void*>(saved)),
+      static_cast<const uint16_t*>(dy), static_cast<uint16_t*>(dx), static_cast<uint16_t*>(dwg), static_cast<uint16_t*>(dwu),
+      static_cast<uint16_t*>(dw2u), bf16_at(workspace, 0), bf16_at(workspace, hidden),
+      reinterpret_cast<float*>(bf16_at(workspace, 2 * hidden)), static_cast<hipStream_t>(stream)));
 }
 
 int hire_pack_mxfp4(const void* w_bf16, int rows, int cols, void* codes, void* scales, void* stream) {

@@ -193,7 +193,8 @@ __global__ __launch_bounds__(64 * MW * NW) __attribute__((amdgpu_waves_per_eu(2,
         for (int j = 0; j < kNB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
     }
   }
-  epi.template store<kMB, kNB>(acc, m0 + wm, n0 + (PAIR ? wn / 2 : wn), g.M, g.N, product, split);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // LDS is the epilogue's
+  epi.store(acc, smem, m0 + wm, n0 + (PAIR ? wn / 2 : wn), g.M, g.N, product, split);
 }
 
 }  // namespace hire

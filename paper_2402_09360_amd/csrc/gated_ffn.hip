@@ -25,35 +25,56 @@ __device__ __forceinline__ float activation(float g, float* slope) {
   }
 }
 
-__device__ __forceinline__ void unpack4(const uint2& v, float (&f)[4]) {
-  f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-}
 __device__ __forceinline__ uint2 pack4(const float (&f)[4]) { return make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3])); }
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  return make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+}
 
-// Four neighbouring columns at a time of a wave's sums: f(row m, column n, quarter of the block, block row, block column).
-template <int MB, int NB, typename F>
-__device__ __forceinline__ void for_quads(int m0, int n0, int M, int N, F f) {
+// A wave's sums in rows: one block of 32 rows after the other goes through LDS (a place per wave, fp32), from where a lane gets
+// eight neighbouring columns of every one of NB blocks that share their columns (PAIRED: all of them), or of one.  Straight
+// from the matrix instruction's layout a lane has four columns of a row: with 8-byte accesses, 32 rows each, the product
+// behind dy took 740 us instead of the 200 of its arithmetic (4096 tokens of d = 2048, 16384 units).
+constexpr int kRowFloats = 68;  // 64 columns and a gap that moves the rows over the banks
+
+// f(row m, column n of the first of eight, values): values[8] of a block column, or [2][8] of both (PAIRED).
+template <bool PAIRED, int MB, int NB, typename F>
+__device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, F f) {
+  static_assert(NB == 2, "64 columns");
   const int lane = lane_id();
+  float* tile = reinterpret_cast<float*>(smem) + wave_id() * 32 * kRowFloats;
+  constexpr int kLanes = PAIRED ? 4 : 8;  // lanes of a row
+  const int col = lane % kLanes * 8;
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
-    const int m = m0 + 32 * i + (lane & 31);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own reads of the block before
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int n = n0 + 32 * j + 8 * q + 4 * (lane >> 5);
-        if (m < M && n < N) f(m, n, q, i, j);
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(tile + (lane & 31) * kRowFloats + 32 * j + 8 * q + 4 * (lane >> 5)) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+      const int r = r0 + lane / kLanes, m = m0 + 32 * i + r, n = n0 + col;
+      float v[PAIRED ? 2 : 1][8];
+#pragma unroll
+      for (int j = 0; j < (PAIRED ? 2 : 1); ++j) {
+        *reinterpret_cast<float4*>(&v[j][0]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col);
+        *reinterpret_cast<float4*>(&v[j][4]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col + 4);
       }
+      if (m < M && n < N) f(m, n, v);
+    }
   }
 }
 
 struct StoreBf16 {
   uint16_t* c[3];
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], int m0, int n0, int M, int N, int product, int) const {
-    for_quads<MB, NB>(m0, n0, M, N, [&](int m, int n, int q, int i, int j) {
-      const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-      *reinterpret_cast<uint2*>(c[product] + (size_t)m * N + n) = pack4(v);
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int product,
+                                        int) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+      *reinterpret_cast<uint4*>(c[product] + (size_t)m * N + n) = pack8(v[0]);
     });
   }
 };
@@ -61,33 +82,65 @@ struct StoreBf16 {
 struct StorePart {  // fp32 sums of one part of k
   float* part;
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], int m0, int n0, int M, int N, int, int split) const {
-    for_quads<MB, NB>(m0, n0, M, N, [&](int m, int n, int q, int i, int j) {
-      *reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n) =
-          make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int,
+                                        int split) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+      float4* to = reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n);
+      to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+      to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
     });
   }
 };
 
-// h = a(g) u; g and u are kept for the backward pass if asked for, rounded to bf16 like h: the matrix cores take no more.
+// What the forward call keeps for the backward one: planes of 16 bits per unit and token.  h is rounded to bf16 as the second
+// product reads it.  g and u keep 24 bits of their fp32 (15 of the significand), the upper 16 in planes of their own and the
+// lower 8 of both in a third: rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to dwg instead
+// of 0.0024 (0.0017 is the rounding of dwg itself).
+struct KeptPlanes {
+  uint16_t *h, *g, *u, *low;
+};
+__device__ __forceinline__ uint32_t upper_pair(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// The second bytes of a g pair and a u pair: g0 u0 g1 u1.
+__device__ __forceinline__ uint32_t lower_pair(float g0, float u0, float g1, float u1) {
+  const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(u0), __float_as_uint(g0), 0x0C0C0501u);
+  return a | __builtin_amdgcn_perm(__float_as_uint(u1), __float_as_uint(g1), 0x05010C0Cu);
+}
+__device__ __forceinline__ void unpack_kept(const uint4& g, const uint4& u, const uint4& low, float (&gv)[8], float (&uv)[8]) {
+  const uint32_t gd[4] = {g.x, g.y, g.z, g.w}, ud[4] = {u.x, u.y, u.z, u.w}, ld[4] = {low.x, low.y, low.z, low.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {  // bytes 0 to 3 of a selector: the second operand's, 4 to 7: the first one's
+    gv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0504000Cu));
+    uv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0504010Cu));
+    gv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0706020Cu));
+    uv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0706030Cu));
+  }
+}
+
+// h = a(g) u.
 template <int ACT>
 struct StoreGated {
-  uint16_t *h, *g, *u;
+  KeptPlanes kept;  // g null: h only
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], int m0, int n0, int M, int N, int, int) const {
-    static_assert(NB == 2, "the gate's block and the other matrix's");
-    for_quads<MB, 1>(m0, n0, M, N, [&](int m, int n, int q, int i, int) {
-      float gv[4], uv[4], hv[4], slope;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        gv[e] = acc[i][0][4 * q + e], uv[e] = acc[i][1][4 * q + e];
-        hv[e] = activation<ACT>(gv[e], &slope) * uv[e];
-      }
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
+    for_rows<true>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[2][8]) {
       const size_t at = (size_t)m * N + n;
-      *reinterpret_cast<uint2*>(h + at) = pack4(hv);
-      if (g) {
-        *reinterpret_cast<uint2*>(g + at) = pack4(gv);
-        *reinterpret_cast<uint2*>(u + at) = pack4(uv);
+      float hv[8], slope;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) hv[e] = activation<ACT>(v[0][e], &slope) * v[1][e];
+      *reinterpret_cast<uint4*>(kept.h + at) = pack8(hv);
+      if (kept.g) {
+        uint32_t g[4], u[4], low[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          g[q] = upper_pair(v[0][2 * q], v[0][2 * q + 1]);
+          u[q] = upper_pair(v[1][2 * q], v[1][2 * q + 1]);
+          low[q] = lower_pair(v[0][2 * q], v[1][2 * q], v[0][2 * q + 1], v[1][2 * q + 1]);
+        }
+        *reinterpret_cast<uint4*>(kept.g + at) = make_uint4(g[0], g[1], g[2], g[3]);
+        *reinterpret_cast<uint4*>(kept.u + at) = make_uint4(u[0], u[1], u[2], u[3]);
+        *reinterpret_cast<uint4*>(kept.low + at) = make_uint4(low[0], low[1], low[2], low[3]);
       }
     });
   }
@@ -96,24 +149,24 @@ struct StoreGated {
 // The sums are dh: dg = dh u a'(g), du = dh a(g), rounded to bf16 for the products that follow.
 template <int ACT>
 struct StoreGateSlopes {
-  const uint16_t *g, *u;
+  KeptPlanes kept;
   uint16_t *dg, *du;
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], int m0, int n0, int M, int N, int, int) const {
-    for_quads<MB, NB>(m0, n0, M, N, [&](int m, int n, int q, int i, int j) {
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
       const size_t at = (size_t)m * N + n;
-      float gv[4], uv[4], dgv[4], duv[4];
-      unpack4(*reinterpret_cast<const uint2*>(g + at), gv);
-      unpack4(*reinterpret_cast<const uint2*>(u + at), uv);
+      float gv[8], uv[8], dgv[8], duv[8];
+      unpack_kept(*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
+                  *reinterpret_cast<const uint4*>(kept.low + at), gv, uv);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 8; ++e) {
         float slope;
-        const float a = activation<ACT>(gv[e], &slope), dh = acc[i][j][4 * q + e];
+        const float a = activation<ACT>(gv[e], &slope), dh = v[0][e];
         dgv[e] = dh * uv[e] * slope;
         duv[e] = dh * a;
       }
-      *reinterpret_cast<uint2*>(dg + at) = pack4(dgv);
-      *reinterpret_cast<uint2*>(du + at) = pack4(duv);
+      *reinterpret_cast<uint4*>(dg + at) = pack8(dgv);
+      *reinterpret_cast<uint4*>(du + at) = pack8(duv);
     });
   }
 };
@@ -181,26 +234,30 @@ size_t gated_part_bytes(int T, int d, int d_ff, int segments) {
   return s > 1 ? (size_t)s * T * d * sizeof(float) : 0;
 }
 
-hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, uint16_t* h, uint16_t* g,
-                                uint16_t* u, float* part, hipStream_t s) {
+namespace {
+KeptPlanes planes_of(const GatedKept& k) { return KeptPlanes{k.h, k.g, k.u, k.low}; }
+}  // namespace
+
+hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
+                                hipStream_t s) {
   GemmArgs up{};
   up.a[0] = x, up.b[0] = L.wg, up.b[1] = L.wu;
   up.M = T, up.N = L.d_ff, up.K = L.d, up.lda = up.ldb = 2u * L.d;
   up.segments = up.products = up.splits = 1;
   const hipError_t e = with_activation(L.act, [&](auto act) {
-    return launch_product<true, true, true>(up, StoreGated<decltype(act)::value>{h, g, u}, s);
+    return launch_product<true, true, true>(up, StoreGated<decltype(act)::value>{planes_of(kept)}, s);
   });
   if (e != hipSuccess) return e;
   GemmArgs down{};
-  down.a[0] = h, down.b[0] = L.w2u;
+  down.a[0] = kept.h, down.b[0] = L.w2u;
   down.M = T, down.N = L.d, down.K = L.d_ff, down.lda = 2u * L.d_ff, down.ldb = 2u * L.d;
   down.segments = 1;
   return launch_split_product<true, false>(down, y, part, s);
 }
 
-hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const uint16_t* g, const uint16_t* u,
-                                 const uint16_t* h, const uint16_t* dy, uint16_t* dx, uint16_t* dwg, uint16_t* dwu,
-                                 uint16_t* dw2u, uint16_t* dg, uint16_t* du, float* part, hipStream_t s) {
+hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
+                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
+                                 float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (dx || dwg || dwu) {
     GemmArgs a{};
@@ -208,7 +265,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
     a.segments = a.products = a.splits = 1;
     e = with_activation(L.act, [&](auto act) {
-      return launch_product<true, true, false>(a, StoreGateSlopes<decltype(act)::value>{g, u, dg, du}, s);
+      return launch_product<true, true, false>(a, StoreGateSlopes<decltype(act)::value>{planes_of(kept), dg, du}, s);
     });
     if (e != hipSuccess) return e;
   }
@@ -219,7 +276,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   };
   add(dg, x, dwg);
   add(du, x, dwu);
-  add(h, dy, dw2u);
+  add(kept.h, dy, dw2u);
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
     w.segments = w.splits = 1;

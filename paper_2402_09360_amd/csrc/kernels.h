@@ -481,13 +481,16 @@ struct GatedLayer {
 };
 // Bytes of the fp32 parts of a product with a T x d result and k = segments * d_ff (0: it is not split).
 size_t gated_part_bytes(int T, int d, int d_ff, int segments);
-// y [T, d]; h [T, d_ff]; g, u (both or neither) likewise: what the backward pass reads.
-hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, uint16_t* h, uint16_t* g,
-                                uint16_t* u, float* part, hipStream_t s);
+// Planes [T, d_ff] of 16 bits that the forward pass leaves for the backward pass; g, u, low null: h only.
+struct GatedKept {
+  uint16_t *h, *g, *u, *low;
+};
+hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
+                                hipStream_t s);
 // dx, dwg, dwu, dw2u: any may be null; dg, du [T, d_ff] scratch.
-hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const uint16_t* g, const uint16_t* u,
-                                 const uint16_t* h, const uint16_t* dy, uint16_t* dx, uint16_t* dwg, uint16_t* dwu,
-                                 uint16_t* dw2u, uint16_t* dg, uint16_t* du, float* part, hipStream_t s);
+hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
+                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
+                                 float* part, hipStream_t s);
 
 // ---- mxfp4.hip: microscaled 4-bit floating point ---------------------------------
 hipError_t launch_pack_mxfp4(const uint16_t* w, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s);

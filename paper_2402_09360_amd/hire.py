@@ -123,13 +123,13 @@ class _GatedLayer(C.Structure):
                 ("act", C.c_int)]
 
 
-for _name in ("hire_gated_ffn_workspace_bytes", "hire_gated_ffn_backward_workspace_bytes"):
+for _name in ("hire_gated_ffn_workspace_bytes", "hire_gated_ffn_saved_bytes", "hire_gated_ffn_backward_workspace_bytes"):
     getattr(_lib, _name).restype = _sz
     getattr(_lib, _name).argtypes = [C.POINTER(_GatedLayer), _i]
 _lib.hire_gated_ffn_step.restype = _i
-_lib.hire_gated_ffn_step.argtypes = [C.POINTER(_GatedLayer), _vp, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.hire_gated_ffn_step.argtypes = [C.POINTER(_GatedLayer), _vp, _i, _vp, _vp, _vp, _sz, _vp]
 _lib.hire_gated_ffn_backward.restype = _i
-_lib.hire_gated_ffn_backward.argtypes = [C.POINTER(_GatedLayer), _vp, _i] + [_vp] * 9 + [_sz, _vp]
+_lib.hire_gated_ffn_backward.argtypes = [C.POINTER(_GatedLayer), _vp, _i] + [_vp] * 7 + [_sz, _vp]
 
 _lib.hire_pack_mxfp4.restype = _lib.hire_unpack_mxfp4.restype = _i
 _lib.hire_pack_mxfp4.argtypes = [_vp, _i, _i, _vp, _vp, _vp]
@@ -571,8 +571,7 @@ class GatedOutputs:
     def __init__(self, layer: GatedLayer, T: int, train: bool = False):
         dev = layer.wg.device
         self.y = torch.empty((T, layer.d_model), dtype=torch.bfloat16, device=dev)
-        self.g, self.u, self.h = (torch.empty((T, layer.d_ff), dtype=torch.bfloat16, device=dev) if train else None
-                                  for _ in range(3))
+        self.saved = (torch.empty(hire_gated_ffn_saved_bytes(layer, T), dtype=torch.uint8, device=dev) if train else None)
 
 
 class GatedGradients:
@@ -588,6 +587,10 @@ def hire_gated_ffn_workspace_bytes(layer: GatedLayer, T: int) -> int:
     return int(_lib.hire_gated_ffn_workspace_bytes(layer.ref, T))
 
 
+def hire_gated_ffn_saved_bytes(layer: GatedLayer, T: int) -> int:
+    return int(_lib.hire_gated_ffn_saved_bytes(layer.ref, T))
+
+
 def hire_gated_ffn_backward_workspace_bytes(layer: GatedLayer, T: int) -> int:
     return int(_lib.hire_gated_ffn_backward_workspace_bytes(layer.ref, T))
 
@@ -596,9 +599,9 @@ def hire_gated_ffn_step(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, w
                         stream=None) -> None:
     """Enqueue the dense gated FFN of x bf16 [T, d_model]."""
     where, bf16, T = "hire_gated_ffn_step", torch.bfloat16, x.shape[0]
-    tokens, hidden = (T, layer.d_model), (T, layer.d_ff)
-    kept = [None if t is None else _tensor(t, bf16, hidden, where) for t in (out.g, out.u, out.h)]
-    _check(_lib.hire_gated_ffn_step(layer.ref, _tensor(x, bf16, tokens, where), T, _tensor(out.y, bf16, tokens, where), *kept,
+    tokens = (T, layer.d_model)
+    saved = None if out.saved is None else _tensor(out.saved, torch.uint8, (hire_gated_ffn_saved_bytes(layer, T),), where)
+    _check(_lib.hire_gated_ffn_step(layer.ref, _tensor(x, bf16, tokens, where), T, _tensor(out.y, bf16, tokens, where), saved,
                                     _ptr(workspace), workspace.numel(), _stream(stream)), where)
 
 
@@ -606,13 +609,13 @@ def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutput
                             grads: GatedGradients, workspace: torch.Tensor, stream=None) -> None:
     """Enqueue the gradients for dy bf16 [T, d_model]; `out` as the forward call with train=True left it."""
     where, bf16, T = "hire_gated_ffn_backward", torch.bfloat16, x.shape[0]
-    tokens, hidden, weights = (T, layer.d_model), (T, layer.d_ff), (layer.d_ff, layer.d_model)
-    if out.g is None:
+    tokens, weights = (T, layer.d_model), (layer.d_ff, layer.d_model)
+    if out.saved is None:
         raise HireError(EINVAL, f"{where}: outputs made with train=True")
-    kept = [_tensor(t, bf16, hidden, where) for t in (out.g, out.u, out.h)]
+    saved = _tensor(out.saved, torch.uint8, (hire_gated_ffn_saved_bytes(layer, T),), where)
     wanted = [None if t is None else _tensor(t, bf16, shape, where)
               for t, shape in ((grads.dx, tokens), (grads.dwg, weights), (grads.dwu, weights), (grads.dw2u, weights))]
-    _check(_lib.hire_gated_ffn_backward(layer.ref, _tensor(x, bf16, tokens, where), T, *kept, _tensor(dy, bf16, tokens, where),
+    _check(_lib.hire_gated_ffn_backward(layer.ref, _tensor(x, bf16, tokens, where), T, saved, _tensor(dy, bf16, tokens, where),
                                         *wanted, _ptr(workspace), workspace.numel(), _stream(stream)), where)
 
 

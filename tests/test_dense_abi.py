@@ -26,18 +26,20 @@ def test_gated_workspaces(hire):
     for T in (1, 16, 64, 65, 1000, 100000):
         assert 0 < fwd(C.byref(gated(hire)), T) and fwd(C.byref(gated(hire)), T) % 256 == 0
         assert bwd(C.byref(gated(hire)), T) >= 2 * T * 16384 * 2
-    for size in (fwd, bwd):
+    saved = hire._lib.hire_gated_ffn_saved_bytes
+    assert saved(C.byref(gated(hire)), 3) == 4 * 3 * 16384 * 2
+    for size in (fwd, bwd, saved):
         assert size(C.byref(gated(hire)), 0) == 0 and size(C.byref(gated(hire)), (1 << 20) + 1) == 0 and size(None, 1) == 0
         for bad, _ in BAD_GATED:
             assert size(C.byref(gated(hire, **bad)), 1) == 0
 
 
 def test_gated_refusals(hire):
-    def step(T=3, x=0x40000, y=0x50000, g=None, u=None, h=None, ws=0x60000, nbytes=256, **layer):
-        return hire._lib.hire_gated_ffn_step(C.byref(gated(hire, **layer)), x, T, y, g, u, h, ws, nbytes, None)
+    def step(T=3, x=0x40000, y=0x50000, saved=None, ws=0x60000, nbytes=256, **layer):
+        return hire._lib.hire_gated_ffn_step(C.byref(gated(hire, **layer)), x, T, y, saved, ws, nbytes, None)
 
-    def back(T=3, x=0x40000, g=0x41000, u=0x42000, h=0x43000, dy=0x44000, outs=(0x45000,) * 4, ws=0x60000, nbytes=256, **layer):
-        return hire._lib.hire_gated_ffn_backward(C.byref(gated(hire, **layer)), x, T, g, u, h, dy, *outs, ws, nbytes, None)
+    def back(T=3, x=0x40000, saved=0x41000, dy=0x44000, outs=(0x45000,) * 4, ws=0x60000, nbytes=256, **layer):
+        return hire._lib.hire_gated_ffn_backward(C.byref(gated(hire, **layer)), x, T, saved, dy, *outs, ws, nbytes, None)
 
     for call in (step, back):
         assert call() == ENOSPC                       # all else is right
@@ -47,14 +49,12 @@ def test_gated_refusals(hire):
             assert call(**{name: None}) == EINVAL and call(**{name: 0x10080}) == EINVAL
         assert call(T=0) == EINVAL and call(T=-1) == EINVAL and call(T=(1 << 20) + 1) == EUNSUPPORTED
         assert call(x=None) == EINVAL and call(x=0x40008) == EINVAL and call(ws=None) == EINVAL and call(ws=0x60010) == EINVAL
+        assert call(saved=0x41080) == EINVAL and call(saved=0x41000) == ENOSPC
     assert step(y=None) == EINVAL and step(y=0x50002) == EINVAL
-    assert step(g=0x1000) == EINVAL and step(g=0x1000, u=0x2000) == EINVAL and step(u=0x1000, h=0x2000) == EINVAL
-    assert step(g=0x1008, u=0x2000, h=0x3000) == EINVAL and step(g=0x1000, u=0x2000, h=0x3000) == ENOSPC
-    for name in ("g", "u", "h", "dy"):
-        assert back(**{name: None}) == EINVAL and back(**{name: 0x1008}) == EINVAL
+    assert back(saved=None) == EINVAL and back(dy=None) == EINVAL and back(dy=0x44008) == EINVAL
     assert back(outs=(None,) * 4) == EINVAL and back(outs=(0x1008, None, None, None)) == EINVAL
     assert back(outs=(None, None, None, 0x1000)) == ENOSPC
-    assert hire._lib.hire_gated_ffn_step(None, 0x40000, 1, 0x50000, None, None, None, 0x60000, 256, None) == EINVAL
+    assert hire._lib.hire_gated_ffn_step(None, 0x40000, 1, 0x50000, None, 0x60000, 256, None) == EINVAL
 
 
 def test_mxfp4_refusals(hire):

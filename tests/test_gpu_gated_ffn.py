@@ -7,6 +7,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 R = 2.0 ** -8      # half a step of bf16, relative
+R24 = 2.0 ** -15  # 24 bits, the rest dropped
 A2 = 0.9           # beyond the largest |a''| of silu (0.5) and of gelu's tanh form (0.80)
 SECOND = 1.03      # products of two or three of the errors above
 
@@ -48,7 +49,7 @@ def expected(x, wg, wu, w2, dy, act):
     dh = dy @ w2.t()
     err_dh = f32(d) * (dy.abs() @ w2.abs().t())
     dg, du = dh * u * da, dh * a
-    kept_g, kept_u = R * g.abs() + err_g, R * u.abs() + err_u
+    kept_g, kept_u = R24 * g.abs() + err_g, R24 * u.abs() + err_u
     err_dg = (R * dg.abs() + err_dh * (u * da).abs() + dh.abs() * (kept_u * da.abs() + u.abs() * a2 * kept_g) +
               2.0 ** -19 * (dh * u).abs() * (1.0 + g.abs()))
     err_du = R * du.abs() + err_dh * a.abs() + dh.abs() * (1.2 * kept_g + 2.0 ** -20 * (a.abs() + g.abs()))
@@ -197,7 +198,9 @@ def test_rows_behind_the_last_stay(hire):
         out = hire.GatedOutputs(layer, T, train=True)
         grads = hire.GatedGradients(layer, T)
         big = {}
-        for o, names in ((out, ("y", "g", "u", "h")), (grads, ("dx", "dwg", "dwu", "dw2u"))):
+        saved = torch.full((out.saved.numel() + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+        out.saved = saved[256:256 + out.saved.numel()]
+        for o, names in ((out, ("y",)), (grads, ("dx", "dwg", "dwu", "dw2u"))):
             for n in names:
                 t = getattr(o, n)
                 big[n] = torch.full((t.shape[0] + 16, t.shape[1]), 7.0, dtype=torch.bfloat16, device="cuda")
@@ -210,7 +213,8 @@ def test_rows_behind_the_last_stay(hire):
         torch.cuda.synchronize()
         for n, t in big.items():
             assert bool((t[:8] == 7.0).all()) and bool((t[-8:] == 7.0).all()), n
-        assert bool((ws[:256] == 0x5A).all()) and bool((ws[256 + nbytes:] == 0x5A).all())
+        for t in (ws, saved):
+            assert bool((t[:256] == 0x5A).all()) and bool((t[-256:] == 0x5A).all())
 
 
 @pytest.mark.parametrize("T", [1, 24, 200])
