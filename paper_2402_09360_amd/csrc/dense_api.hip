@@ -47,7 +47,8 @@ int mx_product(const void* x, const uint8_t* x_scales, int T, const void* w_code
   if (y_type != HIRE_F32 && y_type != HIRE_BF16) return HIRE_EINVAL;
   if (workspace_bytes < hire_mxfp4_product_workspace_bytes(T, rows, cols)) return HIRE_ENOSPC;
   return launched(launch_mx_product(MxProduct{x, x_scales, T, static_cast<const uint8_t*>(w_codes),
-                                              static_cast<const uint8_t*>(w_scales), rows, cols, y, y_type == HIRE_BF16},
+                                              static_cast<const uint8_t*>(w_scales), rows, cols, y, y_type == HIRE_BF16,
+                                              workspace},
                                     static_cast<hipStream_t>(stream)));
 }
 
@@ -130,7 +131,7 @@ int hire_unpack_mxfp4(const void* codes, const void* scales, int rows, int cols,
 
 size_t hire_mxfp4_product_workspace_bytes(int T, int rows, int cols) {
   if (check_mx(T, rows, cols) != HIRE_OK) return 0;
-  return kAlign;
+  return align_up(mx_workspace_bytes(T, rows, cols)) + kAlign;
 }
 
 int hire_mxfp4_product(const void* x_codes, const void* x_scales, int T, const void* w_codes, const void* w_scales, int rows,

@@ -1,0 +1,121 @@
+// What follows the sums of a dense product: rows out of the matrix instruction's layout, stores, parts of k and their join, and
+// the launch.
+#pragma once
+
+#include "dense_gemm.h"
+#include "kernels.h"
+
+namespace hire {
+
+__device__ __forceinline__ uint2 pack4(const float (&f)[4]) { return make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3])); }
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+  return make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
+}
+
+// A wave's sums in rows: one block of 32 rows after the other goes through LDS (a place per wave, fp32), from where a lane gets
+// eight neighbouring columns of every one of NB blocks that share their columns (PAIRED: all of them), or of one.  Straight
+// from the matrix instruction's layout a lane has four columns of a row: with 8-byte accesses, 32 rows each, the product
+// behind dy took 740 us instead of the 200 of its arithmetic (4096 tokens of d = 2048, 16384 units).
+constexpr int kRowFloats = 68;  // 64 columns and a gap that moves the rows over the banks
+
+// f(row m, column n of the first of eight, values): values[8] of a block column, or [2][8] of both (PAIRED).
+template <bool PAIRED, int MB, int NB, typename F>
+__device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, F f) {
+  static_assert(NB == 2, "64 columns");
+  const int lane = lane_id();
+  float* tile = reinterpret_cast<float*>(smem) + wave_id() * 32 * kRowFloats;
+  constexpr int kLanes = PAIRED ? 4 : 8;  // lanes of a row
+  const int col = lane % kLanes * 8;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own reads of the block before
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(tile + (lane & 31) * kRowFloats + 32 * j + 8 * q + 4 * (lane >> 5)) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
+      const int r = r0 + lane / kLanes, m = m0 + 32 * i + r, n = n0 + col;
+      float v[PAIRED ? 2 : 1][8];
+#pragma unroll
+      for (int j = 0; j < (PAIRED ? 2 : 1); ++j) {
+        *reinterpret_cast<float4*>(&v[j][0]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col);
+        *reinterpret_cast<float4*>(&v[j][4]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col + 4);
+      }
+      if (m < M && n < N) f(m, n, v);
+    }
+  }
+}
+
+// fp32 sums of one part of k; N a multiple of 8.
+struct StorePart {
+  float* part;
+  template <int MB, int NB>
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int,
+                                        int split) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+      float4* to = reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n);
+      to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+      to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
+    });
+  }
+};
+
+// Sum of the parts in their order, rounded once to bf16 or left in fp32; values beyond whole fours one by one.
+template <bool BF16>
+__global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ part, void* __restrict__ out, int parts,
+                                                    long long values) {
+  if (values % 4 != 0) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < values; i += (long long)gridDim.x * 256) {
+      float s = part[i];
+      for (int r = 1; r < parts; ++r) s += part[(size_t)r * values + i];
+      if constexpr (BF16)
+        static_cast<__bf16*>(out)[i] = (__bf16)s;
+      else
+        static_cast<float*>(out)[i] = s;
+    }
+    return;
+  }
+  const long long quads = values / 4;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < quads; i += (long long)gridDim.x * 256) {
+    const float4* p = reinterpret_cast<const float4*>(part) + i;
+    float4 s = p[0];
+    for (int r = 1; r < parts; ++r) {
+      const float4 v = p[(size_t)r * quads];
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    if constexpr (BF16) {
+      const float f[4] = {s.x, s.y, s.z, s.w};
+      static_cast<uint2*>(out)[i] = pack4(f);
+    } else {
+      static_cast<float4*>(out)[i] = s;
+    }
+  }
+}
+inline hipError_t launch_join_parts(const float* part, void* out, bool bf16, int parts, long long values, hipStream_t s) {
+  const long long blocks = (values / 4 + 255) / 256 + 1;
+  return launch(bf16 ? &k_join_parts<true> : &k_join_parts<false>, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0,
+                s, part, out, parts, values);
+}
+
+template <bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
+hipError_t launch_product(const GemmArgs& g, const Epilogue& epi, hipStream_t s) {
+  const int n_tile = PAIR ? kGemmTile / 2 : kGemmTile;
+  const long long tiles = (long long)((g.M + kGemmTile - 1) / kGemmTile) * ((g.N + n_tile - 1) / n_tile);
+  return launch(&k_dense_product<AK, BK, PAIR, MX, Epilogue>, dim3((unsigned)(tiles * g.products * g.splits)), dim3(512), 0, s, g,
+                epi);
+}
+
+// Parts of k for a product of one M x N matrix: as many as fill the chip, each at least sixteen stages long.
+inline int product_splits(int M, int N, int steps) {
+  const long long tiles = (long long)((M + kGemmTile - 1) / kGemmTile) * ((N + kGemmTile - 1) / kGemmTile);
+  int s = (int)(256 / tiles);
+  s = s < 1 ? 1 : s;
+  const int most = steps / 16 < 1 ? 1 : steps / 16;
+  return s < most ? s : most;
+}
+
+}  // namespace hire

@@ -5,6 +5,8 @@
 
 #include "device_utils.h"
 
+#include <type_traits>
+
 namespace hire {
 
 typedef float f32x4v __attribute__((ext_vector_type(4)));
@@ -13,7 +15,8 @@ typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
 typedef short s16x4v __attribute__((ext_vector_type(4)));
 
-constexpr int kGemmStep = 64;  // k of one stage: 128 bytes of a k-major row
+constexpr int kGemmStep = 32;    // k of one stage: 64 bytes of a k-major row
+constexpr int kGemmStages = 4;   // in LDS: three on their way or there while one is multiplied
 
 // What loads of a stage that lie behind the end of k read instead.
 __device__ __align__(16) const uint32_t kGemmZeros[4] = {0u, 0u, 0u, 0u};
@@ -30,6 +33,11 @@ __device__ __forceinline__ void gemm_load_at(const void* address, uint32_t lds) 
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(address), "s"(lds) : "memory", "m0");
 }
 
+// The same with four bytes per lane.
+__device__ __forceinline__ void gemm_load_words(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __bf16 v[2] = {(__bf16)lo, (__bf16)hi};  // nearest even
   uint32_t u;
@@ -38,74 +46,77 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 }
 
 // One operand's tile of ROWS m (or n) by kGemmStep k in LDS.
-//   k-major:  [row][128 bytes]; the 16-byte chunk c of row r lies at c ^ (r & 7), so that the rows of a fragment, read at one
-//             chunk, are spread over all banks.
-//   else:     [k][2 ROWS bytes]; the 32-byte unit u of row k lies at u ^ f(k), f taking its values from the bits of k in which
-//             the rows of one transposing read differ.
+//   k-major:  [row][64 bytes]; the 16-byte chunk c of row r lies at c ^ (r / 4 % 4), so that the sixteen rows that a cycle
+//             reads at one chunk are spread over all banks.
+//   else:     [k][2 ROWS bytes]; the 32-byte unit u of row k lies at u ^ 2 (k % 4): half a wave reads four rows of k by two
+//             units.
 // The loads write LDS in order, so the permutation is in the global address.
 // PAIR: rows of two matrices in turn, 32 of the first, 32 of the second (the same rows).
 template <int ROWS, int WAVES, bool KMAJOR, bool PAIR>
 struct GemmTile {
-  static constexpr int kLoads = ROWS * 2 * kGemmStep / (WAVES * 1024);
-  static constexpr int kUnits = ROWS / 16;  // 32-byte units of a row of k
   static constexpr int kBytes = ROWS * 2 * kGemmStep;
-  static_assert(ROWS % 64 == 0 && kLoads * WAVES * 1024 == kBytes, "whole loads");
+  static constexpr int kLoads = kBytes / (WAVES * 1024);
+  static constexpr int kUnits = ROWS / 16;  // 32-byte units of a row of k
+  static_assert(ROWS % 128 == 0 && kLoads * WAVES * 1024 == kBytes, "whole loads");
   uint32_t off[kLoads];
 
-  static __device__ __forceinline__ int f_of_k(int k) { return ((k & 3) | (((k >> 3) & 3) << 2)) & (kUnits - 1); }
+  static __device__ __forceinline__ int unit_of_k(int k) { return (k & 3) << 1; }
+  // The piece (1 KB) of the tile that load i of a wave fills; what of k a lane's 16 bytes of it are.
+  static __device__ __forceinline__ int k_of_lane(int piece) {
+    const int lane = lane_id();
+    return KMAJOR ? ((lane & 3) ^ ((lane >> 4) & 3)) * 8 : piece * (64 / (ROWS / 8)) + lane / (ROWS / 8);
+  }
+  static __device__ __forceinline__ bool second(int piece) { return PAIR && ((piece * 16 / 32) & 1) != 0; }
 
-  // origin: first row of the tile inside a matrix of `extent` rows (PAIR: counts one of the two); ld in bytes.
+  // origin: first row of the tile inside a matrix of `extent` rows (PAIR: counts one of the two); ld in bytes.  Rows behind
+  // the last one repeat it.
   __device__ __forceinline__ void init(int origin, int extent, uint32_t ld) {
     const int wave = wave_id(), lane = lane_id();
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = i * WAVES + wave;  // 1 KB pieces of the tile
+      const int piece = i * WAVES + wave;
       if constexpr (KMAJOR) {
-        int r = at * 8 + lane / 8;
+        int r = piece * 16 + lane / 4;
         if constexpr (PAIR) r = r / 64 * 32 + r % 32;
         r = min(r, extent - 1 - origin);
-        off[i] = (uint32_t)r * ld + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        off[i] = (uint32_t)r * ld + (uint32_t)(k_of_lane(piece) * 2);
       } else {
-        constexpr int kLanes = ROWS / 8;  // lanes of a row
-        const int k = at * (64 / kLanes) + lane / kLanes, pos = lane % kLanes;
-        int chunk = (((pos >> 1) ^ f_of_k(k)) << 1) | (pos & 1);
-        chunk = min(chunk, (extent - 1 - origin) / 8);
-        off[i] = (uint32_t)k * ld + (uint32_t)(chunk * 16);
+        const int k = k_of_lane(piece), pos = lane % (ROWS / 8);
+        const int chunk = (((pos >> 1) ^ unit_of_k(k)) << 1) | (pos & 1);
+        off[i] = (uint32_t)k * ld + (uint32_t)(min(chunk, (extent - 1 - origin) / 8) * 16);
       }
     }
   }
-  // Loads one stage; base: where the tile's first row and k lie (second: of the second matrix, PAIR); left: k from there on.
-  __device__ __forceinline__ void load(const char* base, const char* second, int left, uint32_t lds) const {
-    const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
+  // Requests one stage; base: where the tile's first row and k lie (other: of the second matrix, PAIR); left: k from there on.
+  __device__ __forceinline__ void request(const char* base, const char* other, int left, uint32_t lds, int wave) const {
     if (left >= kGemmStep) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int at = i * WAVES + wave;
-        gemm_load(PAIR && ((at * 8 / 32) & 1) ? second : base, off[i], lds + at * 1024);
+        const int piece = i * WAVES + wave;
+        gemm_load(second(piece) ? other : base, off[i], lds + piece * 1024);
       }
-    } else {
+    } else {  // the last stage of k
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int at = i * WAVES + wave;
-        const char* b = PAIR && ((at * 8 / 32) & 1) ? second : base;
-        const int k = KMAJOR ? ((lane & 7) ^ (lane >> 3)) * 8 : at * (64 / (ROWS / 8)) + lane / (ROWS / 8);
-        gemm_load_at(k < left ? (const void*)(b + off[i]) : (const void*)kGemmZeros, lds + at * 1024);
+        const int piece = i * WAVES + wave;
+        const char* b = second(piece) ? other : base;
+        gemm_load_at(k_of_lane(piece) < left ? (const void*)(b + off[i]) : (const void*)kGemmZeros, lds + piece * 1024);
       }
     }
   }
-  // Eight k (16 ks + 8 (lane / 32) ...) of row `row` + lane % 32 of the tile at `lds` (byte offset).
+  // Eight k (16 ks + 8 (lane / 32) ...) of row `row` + lane % 32 of the tile in LDS.
   static __device__ __forceinline__ bf16x8v fragment(const char* tile, int row, int ks) {
     const int lane = lane_id();
     if constexpr (KMAJOR) {
       const int r = row + (lane & 31), chunk = 2 * ks + (lane >> 5);
-      return *reinterpret_cast<const bf16x8v*>(tile + r * 128 + ((chunk ^ (r & 7)) << 4));
+      return *reinterpret_cast<const bf16x8v*>(tile + r * 64 + ((chunk ^ ((r >> 2) & 3)) << 4));
     } else {
       // sixteen lanes read four rows of k by sixteen columns and get four k of one column each
       const int k = 16 * ks + 8 * (lane >> 5) + ((lane & 15) >> 2), unit = row / 16 + ((lane >> 4) & 1);
-      const char* p = tile + k * (2 * ROWS) + ((unit ^ f_of_k(k)) << 5) + ((lane & 3) << 3);
-      const char* q = tile + (k + 4) * (2 * ROWS) + ((unit ^ f_of_k(k + 4)) << 5) + ((lane & 3) << 3);
+      const char* p = tile + k * (2 * ROWS) + ((unit ^ unit_of_k(k)) << 5) + ((lane & 3) << 3);
       using Lds = __attribute__((address_space(3))) s16x4v*;
-      const s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)q);
+      const s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+      const s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * (2 * ROWS)));  // unit_of_k repeats every four
       bf16x8v v;
       __builtin_memcpy(&v, &lo, 8);
       __builtin_memcpy(reinterpret_cast<char*>(&v) + 8, &hi, 8);
@@ -113,6 +124,14 @@ struct GemmTile {
     }
   }
 };
+
+// A block of 32 codes as the matrix instruction takes it.
+typedef int i32x8v __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ i32x8v mx_codes(const bf16x8v& block) {
+  int d[4];
+  __builtin_memcpy(d, &block, 16);
+  return i32x8v{d[0], d[1], d[2], d[3], 0, 0, 0, 0};
+}
 
 struct GemmArgs {
   const void* a[3];  // by segment of k, or by product
@@ -122,6 +141,10 @@ struct GemmArgs {
   int segments;      // > 1: k runs over a[0] b[0], then a[1] b[1], ...
   int products;      // > 1: so many products of one shape
   int splits;        // parts of k, whose sums the epilogue gets apart
+  // microscaled operands only (a[0], b[0]: 4-bit codes, K in quarters of a column): scale bytes [M, scale_ld], [N, scale_ld],
+  // scale_ld a multiple of 4 (bytes behind the last block: 127)
+  const uint8_t *a_scales, *b_scales;
+  uint32_t scale_ld;
 };
 
 // Place of workgroup `w` of `total`: consecutive places on one die (workgroups go to the eight dies in turn), so that the
@@ -131,68 +154,152 @@ __device__ __forceinline__ int gemm_place(int w, int total) {
   return die * each + min(die, rest) + (w >> 3);
 }
 
-// The tile of MT x NT by MW x NW waves; two stages in LDS: while one is multiplied the next one is on its way.
+// Workgroup barriers that no instruction is moved across.
+__device__ __forceinline__ void gemm_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// A tile of 256 x 256 by eight waves of 128 x 64, two on every SIMD.  The waves work in two groups half a stage apart: while one
+// group's matrix instructions run, the other reads its fragments of a whole stage, requests the stage three ahead and waits;
+// then they change places.  Per stage of 32 k a wave reads 12 KB of LDS and issues 16 matrix instructions of 32 cycles, so the
+// reads of four waves (48 KB at 256 bytes a cycle) hide behind the others' 512 cycles.
+//   Places in LDS: stage s lies in place s % 4.  The stage requested while s is read, s + 3, goes where s - 1 was, whose last
+// reader is the second group one barrier earlier.  Before a wave passes the barrier behind its reads of stage s, its own loads
+// of stage s + 1 have arrived (two younger stages may be on their way), and the group that reads s + 1 first does so behind a
+// barrier that all waves passed with that wait done.
+//   Measured against a double buffer of 64 k whose waves run freely (4096 x 4096 x 8192, normal values): 1019 -> 1222
+// TFLOP/s; 79 % of the cycles are the matrix cores' (56 %), and with these values the clock drops to about 1.6 GHz: with
+// zeros the same kernel does 1665.
 // An epilogue gets a wave's sums: acc[i][j], rows m of block i at lane % 32, columns n of block j: register r is column
 // 8 (r / 4) + 4 (lane / 32) + r % 4.
-template <int MT, int NT, int MW, int NW, bool AK, bool BK, bool PAIR, class Epilogue>
-__global__ __launch_bounds__(64 * MW * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_product(GemmArgs g, Epilogue epi) {
-  constexpr int kWaves = MW * NW, kMB = MT / MW / 32, kNB = NT / NW / 32;
-  using TA = GemmTile<MT, kWaves, AK, false>;
-  using TB = GemmTile<NT, kWaves, BK, PAIR>;
-  constexpr int kStage = TA::kBytes + TB::kBytes;
-  __shared__ __align__(1024) char smem[2 * kStage];
+// MX: microscaled operands.  A stage's 64 bytes of a row are 128 columns, four blocks; the row's four scale bytes travel beside
+// them, one word per row of both tiles.  A lane's sixteen bytes of a fragment are one block, whose scale byte the matrix
+// instruction picks from the row's word, shifted by a byte in the upper half of the wave.
+constexpr int kGemmTile = 256;
+template <bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_product(GemmArgs g, Epilogue epi) {
+  constexpr int kWaves = 8, kMB = 4, kNB = 2;
+  using TA = GemmTile<kGemmTile, kWaves, AK, false>;
+  using TB = GemmTile<kGemmTile, kWaves, BK, PAIR>;
+  static_assert(!MX || (AK && BK && !PAIR), "rows of codes");
+  constexpr int kCodes = TA::kBytes + TB::kBytes, kStage = kCodes + (MX ? 2 * kGemmTile * 4 : 0);
+  constexpr int kYounger = (kGemmStages - 2) * (TA::kLoads + TB::kLoads + (MX ? 1 : 0));
+  __shared__ __align__(1024) char smem[kGemmStages * kStage];
 
-  const int n_tile = PAIR ? NT / 2 : NT;
-  const int tiles_m = (g.M + MT - 1) / MT, tiles_n = (g.N + n_tile - 1) / n_tile, tiles = tiles_m * tiles_n;
+  const int n_tile = PAIR ? kGemmTile / 2 : kGemmTile;
+  const int tiles_m = (g.M + kGemmTile - 1) / kGemmTile, tiles_n = (g.N + n_tile - 1) / n_tile, tiles = tiles_m * tiles_n;
   const int w = gemm_place((int)blockIdx.x, (int)gridDim.x), z = w / tiles, t = w % tiles;
   const int product = z / g.splits, split = z % g.splits;
   // groups of eight tiles of m, so that the 32 workgroups of a die form a patch
   const int group = t / (8 * tiles_n), in = t % (8 * tiles_n), gm = min(8, tiles_m - 8 * group);
-  const int m0 = (8 * group + in % gm) * MT, n0 = in / gm * n_tile;
+  const int m0 = (8 * group + in % gm) * kGemmTile, n0 = in / gm * n_tile;
 
   const int seg_steps = (g.K + kGemmStep - 1) / kGemmStep, steps = seg_steps * g.segments;
-  const int s0 = (int)((long long)steps * split / g.splits), s1 = (int)((long long)steps * (split + 1) / g.splits);
+  const int s0 = (int)((long long)steps * split / g.splits);
+  const int n = (int)((long long)steps * (split + 1) / g.splits) - s0;
 
   TA ta;
   TB tb;
   ta.init(m0, g.M, g.lda);
   tb.init(n0, g.N, g.ldb);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
-  auto request = [&](int s) {
-    const int seg = s / seg_steps, k = (s - seg * seg_steps) * kGemmStep, left = g.K - k;
-    const int which = g.segments > 1 ? seg : product;
-    const size_t ka = AK ? (size_t)m0 * g.lda + 2 * (size_t)k : (size_t)k * g.lda + 2 * (size_t)m0;
-    const size_t kb = BK ? (size_t)n0 * g.ldb + 2 * (size_t)k : (size_t)k * g.ldb + 2 * (size_t)n0;
-    const uint32_t lds = lds0 + (uint32_t)((s - s0) & 1) * kStage;
-    ta.load(static_cast<const char*>(g.a[which]) + ka, nullptr, left, lds);
-    if constexpr (PAIR)
-      tb.load(static_cast<const char*>(g.b[0]) + kb, static_cast<const char*>(g.b[1]) + kb, left, lds + TA::kBytes);
-    else
-      tb.load(static_cast<const char*>(g.b[which]) + kb, nullptr, left, lds + TA::kBytes);
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id());
+  const char* scales = nullptr;  // MX: waves 0 to 3 those of the first tile's rows, 4 to 7 of the second's
+  uint32_t scale_off = 0;
+  if constexpr (MX) {
+    const int row0 = wave < 4 ? m0 : n0, last = (wave < 4 ? g.M : g.N) - 1 - row0;
+    scales = reinterpret_cast<const char*>(wave < 4 ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld + 4 * (size_t)s0;
+    scale_off = (uint32_t)min(wave % 4 * 64 + lane_id(), last) * g.scale_ld;
+  }
+  // the next stage to request: its place, addresses and what is left of its segment of k
+  int requested = 0, place = 0, left = 0;
+  const char *pa = nullptr, *pb = nullptr, *pb2 = nullptr;
+  auto locate = [&](int s) {
+    const int seg = s / seg_steps, k = (s - seg * seg_steps) * kGemmStep, which = g.segments > 1 ? seg : product;
+    left = g.K - k;
+    pa = static_cast<const char*>(g.a[which]) + (AK ? (size_t)m0 * g.lda + 2 * (size_t)k : (size_t)k * g.lda + 2 * (size_t)m0);
+    const size_t at = BK ? (size_t)n0 * g.ldb + 2 * (size_t)k : (size_t)k * g.ldb + 2 * (size_t)n0;
+    pb = static_cast<const char*>(g.b[PAIR ? 0 : which]) + at;
+    if constexpr (PAIR) pb2 = static_cast<const char*>(g.b[1]) + at;
+  };
+  auto request = [&]() {
+    const uint32_t lds = lds0 + (uint32_t)place * kStage;
+    ta.request(pa, nullptr, left, lds, wave);
+    tb.request(pb, pb2, left, lds + TA::kBytes, wave);
+    if constexpr (MX) {
+      gemm_load_words(scales, scale_off, lds + kCodes + wave * 256);
+      scales += 4;
+    }
+    place = place + 1 == kGemmStages ? 0 : place + 1;
+    left -= kGemmStep;
+    pa += AK ? 2 * kGemmStep : (size_t)kGemmStep * g.lda;
+    const size_t next = BK ? 2 * kGemmStep : (size_t)kGemmStep * g.ldb;
+    pb += next;
+    if constexpr (PAIR) pb2 += next;
+    if (++requested < n && left <= 0) locate(s0 + requested);
   };
 
-  const int wave = wave_id(), wm = wave / NW * (MT / MW), wn = wave % NW * (NT / NW);
+  const int wm = wave / 4 * 128, wn = wave % 4 * 64;
   f32x16v acc[kMB][kNB] = {};
-  if (s0 < s1) request(s0);
-  for (int s = s0; s < s1; ++s) {
-    // this stage has arrived for every wave, and nobody reads the other one any more
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (s + 1 < s1) request(s + 1);
-    const char* sa = smem + ((s - s0) & 1) * kStage;
+  if (n > 0) locate(s0);
+  for (int i = 0; i < kGemmStages - 1 && i < n; ++i) request();
+  if (n >= kGemmStages - 1)
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kYounger) : "memory");
+  else
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  if (wave >= 4) gemm_barrier();  // the second group: half a stage later
+  int cur = 0;
+  for (int s = 0; s < n; ++s) {
+    const char* sa = smem + cur * kStage;
     const char* sb = sa + TA::kBytes;
+    cur = cur + 1 == kGemmStages ? 0 : cur + 1;
+    bf16x8v fa[2][kMB], fb[2][kNB];
 #pragma unroll
-    for (int ks = 0; ks < kGemmStep / 16; ++ks) {
-      bf16x8v fa[kMB], fb[kNB];
+    for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-      for (int i = 0; i < kMB; ++i) fa[i] = TA::fragment(sa, wm + 32 * i, ks);
+      for (int j = 0; j < kNB; ++j) fb[ks][j] = TB::fragment(sb, wn + 32 * j, ks);
 #pragma unroll
-      for (int j = 0; j < kNB; ++j) fb[j] = TB::fragment(sb, wn + 32 * j, ks);
+      for (int i = 0; i < kMB; ++i) fa[ks][i] = TA::fragment(sa, wm + 32 * i, ks);
+    }
+    uint32_t xa[kMB], xb[kNB];  // MX: bytes 0 and 2 are the scales of this lane's blocks
+    if constexpr (MX) {
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(sa + kCodes) + (lane_id() & 31);
+      const int shift = lane_id() >> 5 << 3;
+#pragma unroll
+      for (int i = 0; i < kMB; ++i) xa[i] = words[wm + 32 * i] >> shift;
+#pragma unroll
+      for (int j = 0; j < kNB; ++j) xb[j] = words[kGemmTile + wn + 32 * j] >> shift;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (requested < n) {
+      request();
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kYounger) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    }
+    gemm_barrier();
+    __builtin_amdgcn_s_setprio(1);
+    auto multiply = [&](auto half) {
+      constexpr int KS = decltype(half)::value;
 #pragma unroll
       for (int i = 0; i < kMB; ++i)
 #pragma unroll
-        for (int j = 0; j < kNB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    }
+        for (int j = 0; j < kNB; ++j) {
+          if constexpr (MX)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(mx_codes(fb[KS][j]), mx_codes(fa[KS][i]), acc[i][j], 4, 4,
+                                                                        2 * KS, (int)xb[j], 2 * KS, (int)xa[i]);
+          else
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[KS][j], fa[KS][i], acc[i][j], 0, 0, 0);
+        }
+    };
+    multiply(std::integral_constant<int, 0>{});
+    multiply(std::integral_constant<int, 1>{});
+    __builtin_amdgcn_s_setprio(0);
+    gemm_barrier();
   }
+  if (wave < 4) gemm_barrier();
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // LDS is the epilogue's
   epi.store(acc, smem, m0 + wm, n0 + (PAIR ? wn / 2 : wn), g.M, g.N, product, split);
 }

@@ -1,8 +1,6 @@
 // The dense gated FFN, forward and backward, for any number of tokens.
-#include "dense_gemm.h"
+#include "dense_epilogue.h"
 #include "kernels.h"
-
-#include <type_traits>
 
 namespace hire {
 namespace {
@@ -25,49 +23,6 @@ __device__ __forceinline__ float activation(float g, float* slope) {
   }
 }
 
-__device__ __forceinline__ uint2 pack4(const float (&f)[4]) { return make_uint2(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3])); }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-  return make_uint4(bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]), bf16_pair(f[6], f[7]));
-}
-
-// A wave's sums in rows: one block of 32 rows after the other goes through LDS (a place per wave, fp32), from where a lane gets
-// eight neighbouring columns of every one of NB blocks that share their columns (PAIRED: all of them), or of one.  Straight
-// from the matrix instruction's layout a lane has four columns of a row: with 8-byte accesses, 32 rows each, the product
-// behind dy took 740 us instead of the 200 of its arithmetic (4096 tokens of d = 2048, 16384 units).
-constexpr int kRowFloats = 68;  // 64 columns and a gap that moves the rows over the banks
-
-// f(row m, column n of the first of eight, values): values[8] of a block column, or [2][8] of both (PAIRED).
-template <bool PAIRED, int MB, int NB, typename F>
-__device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, F f) {
-  static_assert(NB == 2, "64 columns");
-  const int lane = lane_id();
-  float* tile = reinterpret_cast<float*>(smem) + wave_id() * 32 * kRowFloats;
-  constexpr int kLanes = PAIRED ? 4 : 8;  // lanes of a row
-  const int col = lane % kLanes * 8;
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own reads of the block before
-#pragma unroll
-    for (int j = 0; j < NB; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4*>(tile + (lane & 31) * kRowFloats + 32 * j + 8 * q + 4 * (lane >> 5)) =
-            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-      const int r = r0 + lane / kLanes, m = m0 + 32 * i + r, n = n0 + col;
-      float v[PAIRED ? 2 : 1][8];
-#pragma unroll
-      for (int j = 0; j < (PAIRED ? 2 : 1); ++j) {
-        *reinterpret_cast<float4*>(&v[j][0]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col);
-        *reinterpret_cast<float4*>(&v[j][4]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col + 4);
-      }
-      if (m < M && n < N) f(m, n, v);
-    }
-  }
-}
-
 struct StoreBf16 {
   uint16_t* c[3];
   template <int MB, int NB>
@@ -75,19 +30,6 @@ struct StoreBf16 {
                                         int) const {
     for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
       *reinterpret_cast<uint4*>(c[product] + (size_t)m * N + n) = pack8(v[0]);
-    });
-  }
-};
-
-struct StorePart {  // fp32 sums of one part of k
-  float* part;
-  template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int,
-                                        int split) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
-      float4* to = reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n);
-      to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
-      to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
     });
   }
 };
@@ -171,53 +113,14 @@ struct StoreGateSlopes {
   }
 };
 
-// Sum of the parts in their order, rounded once.
-__global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ part, uint16_t* __restrict__ out, int parts,
-                                                    long long quads) {
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < quads; i += (long long)gridDim.x * 256) {
-    const float4* p = reinterpret_cast<const float4*>(part) + i;
-    float4 s = p[0];
-    for (int r = 1; r < parts; ++r) {
-      const float4 v = p[(size_t)r * quads];
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    const float f[4] = {s.x, s.y, s.z, s.w};
-    reinterpret_cast<uint2*>(out)[i] = pack4(f);
-  }
-}
-
-constexpr int kTile = 256;
-
-template <bool AK, bool BK, bool PAIR, class Epilogue>
-hipError_t launch_product(const GemmArgs& g, const Epilogue& epi, hipStream_t s) {
-  auto* kernel = &k_dense_product<kTile, kTile, 2, 4, AK, BK, PAIR, Epilogue>;
-  const int n_tile = PAIR ? kTile / 2 : kTile;
-  const long long tiles = (long long)((g.M + kTile - 1) / kTile) * ((g.N + n_tile - 1) / n_tile);
-  return launch(kernel, dim3((unsigned)(tiles * g.products * g.splits)), dim3(512), 0, s, g, epi);
-}
-
-// Parts of k for a product of one M x N matrix: as many as fill the chip, each at least eight stages long.
-int product_splits(int M, int N, int steps) {
-  const long long tiles = (long long)((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
-  int s = (int)(256 / tiles);
-  s = s < 1 ? 1 : s;
-  const int most = steps / 8 < 1 ? 1 : steps / 8;
-  return s < most ? s : most;
-}
-
-hipError_t launch_join(const float* part, uint16_t* out, int parts, long long values, hipStream_t s) {
-  const long long quads = values / 4, blocks = (quads + 255) / 256;
-  return launch(&k_join_parts, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, part, out, parts, quads);
-}
-
 // One product with an M x N bf16 result, split over k where the tiles are few.
 template <bool AK, bool BK>
 hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStream_t s) {
   g.products = 1;
   g.splits = product_splits(g.M, g.N, g.segments * ((g.K + kGemmStep - 1) / kGemmStep));
-  if (g.splits == 1) return launch_product<AK, BK, false>(g, StoreBf16{{out, nullptr, nullptr}}, s);
-  const hipError_t e = launch_product<AK, BK, false>(g, StorePart{part}, s);
-  return e != hipSuccess ? e : launch_join(part, out, g.splits, (long long)g.M * g.N, s);
+  if (g.splits == 1) return launch_product<AK, BK, false, false>(g, StoreBf16{{out, nullptr, nullptr}}, s);
+  const hipError_t e = launch_product<AK, BK, false, false>(g, StorePart{part}, s);
+  return e != hipSuccess ? e : launch_join_parts(part, out, true, g.splits, (long long)g.M * g.N, s);
 }
 
 template <typename F>
@@ -245,7 +148,7 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
   up.M = T, up.N = L.d_ff, up.K = L.d, up.lda = up.ldb = 2u * L.d;
   up.segments = up.products = up.splits = 1;
   const hipError_t e = with_activation(L.act, [&](auto act) {
-    return launch_product<true, true, true>(up, StoreGated<decltype(act)::value>{planes_of(kept)}, s);
+    return launch_product<true, true, true, false>(up, StoreGated<decltype(act)::value>{planes_of(kept)}, s);
   });
   if (e != hipSuccess) return e;
   GemmArgs down{};
@@ -265,7 +168,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
     a.segments = a.products = a.splits = 1;
     e = with_activation(L.act, [&](auto act) {
-      return launch_product<true, true, false>(a, StoreGateSlopes<decltype(act)::value>{planes_of(kept), dg, du}, s);
+      return launch_product<true, true, false, false>(a, StoreGateSlopes<decltype(act)::value>{planes_of(kept), dg, du}, s);
     });
     if (e != hipSuccess) return e;
   }
@@ -280,7 +183,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
     w.segments = w.splits = 1;
-    e = launch_product<false, false, false>(w, out, s);
+    e = launch_product<false, false, false, false>(w, out, s);
     if (e != hipSuccess) return e;
   }
   if (dx) {

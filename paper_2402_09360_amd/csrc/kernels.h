@@ -505,7 +505,9 @@ struct MxProduct {
   int rows, cols;
   void* y;                  // [T, rows], bf16 or fp32
   int y_bf16;
+  void* workspace;          // mx_workspace_bytes
 };
+size_t mx_workspace_bytes(int T, int rows, int cols);
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s);
 
 // ---- verify.hip: drafted tokens against the target's probabilities ----------------

@@ -2,11 +2,10 @@
 // 4, 6 and their negatives) times the block's power of two, an e8m0 byte (2^(byte - 127); 255: not a number).
 #pragma once
 
-#include "device_utils.h"
+#include "dense_gemm.h"
 
 namespace hire {
 
-typedef int i32x8v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
 constexpr int kMxBlock = 32;

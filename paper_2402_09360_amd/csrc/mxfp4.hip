@@ -2,10 +2,7 @@
 // themselves.  Layout: codes [rows, cols / 2], the lower column in the low nibble; scale bytes [rows, cols / 32].
 #include "mxfp4.h"
 
-#include "dense_gemm.h"
-#include "kernels.h"
-
-#include <type_traits>
+#include "dense_epilogue.h"
 
 namespace hire {
 namespace {
@@ -155,127 +152,45 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx_few(const uint8_t* __rest
 }
 
 // ---- many tokens, packed ----------------------------------------------------------
-// Tiles as in the product of bf16 matrices: 128 bytes of a row are a stage of 256 columns, 16 of them a block and what a lane
-// holds of the matrix instruction.  A row's eight scale bytes of a stage come straight into registers of the lanes that
-// need them, requested with the stage.
-constexpr int kMxStage = 256;
-
-__device__ __forceinline__ uint2 stage_scales(const uint8_t* row, int block, int blocks) {
-  uint2 v;
-  if (block + 8 <= blocks) {
-    __builtin_memcpy(&v, row + block, 8);
-    return v;
+// y's rows out of the sums: whole vectors where the row length admits them.
+struct StoreProduct {
+  void* y;
+  int bf16;
+  template <int MB, int NB>
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+      const size_t at = (size_t)m * N + n;
+      if (N % 8 != 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < N) {
+            if (bf16)
+              static_cast<__bf16*>(y)[at + e] = (__bf16)v[0][e];
+            else
+              static_cast<float*>(y)[at + e] = v[0][e];
+          }
+      } else if (bf16) {
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(y) + at) = pack8(v[0]);
+      } else {
+        float4* to = reinterpret_cast<float4*>(static_cast<float*>(y) + at);
+        to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
+        to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
+      }
+    });
   }
-  uint32_t d[2] = {0x7F7F7F7Fu, 0x7F7F7F7Fu};  // 1 behind the end, where the codes are 0
-  for (int i = 0; i < 8; ++i)
-    if (block + i < blocks) d[i / 4] = (d[i / 4] & ~(0xFFu << (8 * (i % 4)))) | (uint32_t)row[block + i] << (8 * (i % 4));
-  return make_uint2(d[0], d[1]);
-}
+};
 
-template <int KS>
-__device__ __forceinline__ f32x16v mx_mfma(const i32x8v& a, const i32x8v& b, const f32x16v& c, uint32_t sa, uint32_t sb) {
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, KS, (int)sa, KS, (int)sb);
-}
-
-template <int MT, int NT, int MW, int NW>
-__global__ __launch_bounds__(64 * MW * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_mx_product(
-    const uint8_t* __restrict__ x, const uint8_t* __restrict__ x_scales, int T, const uint8_t* __restrict__ codes,
-    const uint8_t* __restrict__ scales, int rows, int cols, void* __restrict__ y, int y_bf16) {
-  constexpr int kWaves = MW * NW, kMB = MT / MW / 32, kNB = NT / NW / 32;
-  using TA = GemmTile<MT, kWaves, true, false>;
-  using TB = GemmTile<NT, kWaves, true, false>;
-  constexpr int kStage = TA::kBytes + TB::kBytes;
-  __shared__ __align__(1024) char smem[2 * kStage];
-
-  const int tiles_m = (T + MT - 1) / MT, tiles_n = (rows + NT - 1) / NT, blocks = cols / kMxBlock;
-  const int t = gemm_place((int)blockIdx.x, (int)gridDim.x);
-  const int group = t / (8 * tiles_n), in = t % (8 * tiles_n), gm = min(8, tiles_m - 8 * group);
-  const int m0 = (8 * group + in % gm) * MT, n0 = in / gm * NT;
-  const uint32_t ld = (uint32_t)cols / 2;
-  const int steps = (cols + kMxStage - 1) / kMxStage;
-
-  TA ta;
-  TB tb;
-  ta.init(m0, T, ld);
-  tb.init(n0, rows, ld);
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
-  const int wave = wave_id(), lane = lane_id(), wm = wave / NW * (MT / MW), wn = wave % NW * (NT / NW);
-  const uint8_t *xs[kMB], *ws[kNB];
+// Scale bytes in rows of whole words, 127 behind the last block: what the product reads where the columns are no multiple of
+// 128 (or the caller's bytes start between words).
+__global__ __launch_bounds__(256) void k_pad_scales(const uint8_t* __restrict__ scales, long long rows, int blocks, int words,
+                                                    uint32_t* __restrict__ out) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (long long)gridDim.x * 256) {
+    const long long row = i / words;
+    const int b = (int)(i - row * words) * 4;
+    uint32_t v = 0u;
 #pragma unroll
-  for (int i = 0; i < kMB; ++i) xs[i] = x_scales + (size_t)min(m0 + wm + 32 * i + (lane & 31), T - 1) * blocks;
-#pragma unroll
-  for (int j = 0; j < kNB; ++j) ws[j] = scales + (size_t)min(n0 + wn + 32 * j + (lane & 31), rows - 1) * blocks;
-  uint2 nx[kMB], nw[kNB];
-  auto request = [&](int s) {
-    const uint32_t lds = lds0 + (uint32_t)(s & 1) * kStage;
-    const int left = (cols - s * kMxStage) / 4;  // the tile counts two bytes as one of 64
-    ta.load(reinterpret_cast<const char*>(x) + (size_t)m0 * ld + (size_t)s * 128, nullptr, left, lds);
-    tb.load(reinterpret_cast<const char*>(codes) + (size_t)n0 * ld + (size_t)s * 128, nullptr, left, lds + TA::kBytes);
-#pragma unroll
-    for (int i = 0; i < kMB; ++i) nx[i] = stage_scales(xs[i], 8 * s, blocks);
-#pragma unroll
-    for (int j = 0; j < kNB; ++j) nw[j] = stage_scales(ws[j], 8 * s, blocks);
-  };
-  // bytes of the blocks 0 2 4 6 for the lower half of the wave, 1 3 5 7 for the upper one
-  const uint32_t pick = lane < 32 ? 0x06040200u : 0x07050301u;
-
-  f32x16v acc[kMB][kNB] = {};
-  request(0);
-  for (int s = 0; s < steps; ++s) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    uint32_t sx[kMB], sw[kNB];
-#pragma unroll
-    for (int i = 0; i < kMB; ++i) {
-      sx[i] = __builtin_amdgcn_perm(nx[i].y, nx[i].x, pick);
-      asm volatile("" : "+v"(sx[i]));  // before the next stage's requests: behind them the compiler would wait for those
-    }
-#pragma unroll
-    for (int j = 0; j < kNB; ++j) {
-      sw[j] = __builtin_amdgcn_perm(nw[j].y, nw[j].x, pick);
-      asm volatile("" : "+v"(sw[j]));
-    }
-    if (s + 1 < steps) request(s + 1);
-    const char* sa = smem + (s & 1) * kStage;
-    const char* sb = sa + TA::kBytes;
-    auto multiply = [&](auto ks) {
-      constexpr int KS = decltype(ks)::value;
-      i32x8v fa[kMB] = {}, fb[kNB] = {};
-#pragma unroll
-      for (int i = 0; i < kMB; ++i) {
-        const bf16x8v v = TA::fragment(sa, wm + 32 * i, KS);
-        __builtin_memcpy(&fa[i], &v, 16);
-      }
-#pragma unroll
-      for (int j = 0; j < kNB; ++j) {
-        const bf16x8v v = TB::fragment(sb, wn + 32 * j, KS);
-        __builtin_memcpy(&fb[j], &v, 16);
-      }
-#pragma unroll
-      for (int i = 0; i < kMB; ++i)
-#pragma unroll
-        for (int j = 0; j < kNB; ++j) acc[i][j] = mx_mfma<KS>(fb[j], fa[i], acc[i][j], sw[j], sx[i]);
-    };
-    multiply(std::integral_constant<int, 0>{});
-    multiply(std::integral_constant<int, 1>{});
-    multiply(std::integral_constant<int, 2>{});
-    multiply(std::integral_constant<int, 3>{});
-  }
-#pragma unroll
-  for (int i = 0; i < kMB; ++i) {
-    const int m = m0 + wm + 32 * i + (lane & 31);
-#pragma unroll
-    for (int j = 0; j < kNB; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = n0 + wn + 32 * j + 8 * (r / 4) + 4 * (lane >> 5) + r % 4;
-        if (m < T && n < rows) {
-          const size_t o = (size_t)m * rows + n;
-          if (y_bf16)
-            static_cast<__bf16*>(y)[o] = (__bf16)acc[i][j][r];
-          else
-            static_cast<float*>(y)[o] = acc[i][j][r];
-        }
-      }
+    for (int e = 0; e < 4; ++e) v |= (b + e < blocks ? (uint32_t)scales[row * blocks + b + e] : 127u) << (8 * e);
+    out[i] = v;
   }
 }
 
@@ -306,11 +221,39 @@ hipError_t launch_unpack_mxfp4(const uint8_t* codes, const uint8_t* scales, int 
                 reinterpret_cast<const uint32_t*>(codes), scales, eights, reinterpret_cast<uint4*>(w));
 }
 
+namespace {
+bool mx_pads_scales(const MxProduct& p) {
+  return p.cols % 128 != 0 || reinterpret_cast<uintptr_t>(p.x_scales) % 4 != 0 || reinterpret_cast<uintptr_t>(p.scales) % 4 != 0;
+}
+}  // namespace
+
+// Room for the padded scale bytes, whether this call's pointers need them or not.
+size_t mx_workspace_bytes(int T, int rows, int cols) {
+  return T <= kMxFewTokens ? 0 : ((size_t)T + rows) * ((cols / kMxBlock + 3) / 4) * 4;
+}
+
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
   if (p.T <= kMxFewTokens) return p.x_scales ? launch_few_tokens<true>(p, s) : launch_few_tokens<false>(p, s);
-  const long long tiles = (long long)((p.T + 255) / 256) * ((p.rows + 255) / 256);
-  return launch(&k_mx_product<256, 256, 2, 4>, dim3((unsigned)tiles), dim3(512), 0, s, static_cast<const uint8_t*>(p.x), p.x_scales,
-                p.T, p.codes, p.scales, p.rows, p.cols, p.y, p.y_bf16);
+  const int blocks = p.cols / kMxBlock, words = (blocks + 3) / 4;
+  GemmArgs g{};
+  g.a[0] = p.x, g.b[0] = p.codes;
+  g.M = p.T, g.N = p.rows, g.K = p.cols / 4, g.lda = g.ldb = (uint32_t)p.cols / 2;
+  g.segments = g.products = g.splits = 1;
+  g.a_scales = p.x_scales, g.b_scales = p.scales, g.scale_ld = 4u * words;
+  if (mx_pads_scales(p)) {
+    uint32_t* padded = static_cast<uint32_t*>(p.workspace);
+    auto pad = [&](const uint8_t* from, int rows, uint32_t* to) {
+      const long long groups = ((long long)rows * words + 255) / 256;
+      return launch(&k_pad_scales, dim3((unsigned)(groups < 4096 ? groups : 4096)), dim3(256), 0, s, from, (long long)rows, blocks,
+                    words, to);
+    };
+    hipError_t e = pad(p.x_scales, p.T, padded);
+    if (e == hipSuccess) e = pad(p.scales, p.rows, padded + (size_t)p.T * words);
+    if (e != hipSuccess) return e;
+    g.a_scales = reinterpret_cast<const uint8_t*>(padded);
+    g.b_scales = reinterpret_cast<const uint8_t*>(padded + (size_t)p.T * words);
+  }
+  return launch_product<true, true, false, true>(g, StoreProduct{p.y, p.y_bf16}, s);
 }
 
 }  // namespace hire
