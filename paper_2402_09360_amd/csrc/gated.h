@@ -1,0 +1,57 @@
+// What the kernels of the dense gated FFN share: the activation and its derivative, and the planes kept for the backward pass.
+#pragma once
+
+#include "dense_epilogue.h"
+
+namespace hire {
+
+// Activation a(g) and its derivative.  silu and the tanh form of gelu are both g s(z) with the logistic function s:
+// z = g, or 2 sqrt(2/pi) (g + 0.044715 g^3).  a' = s + g s (1 - s) z'.
+constexpr float kGelu = 1.5957691216057308f, kGeluCube = 0.044715f, kLog2E = 1.4426950408889634f;
+template <int ACT>
+__device__ __forceinline__ float activation(float g, float* slope) {
+  if constexpr (ACT == kActRelu) {
+    *slope = g > 0.0f ? 1.0f : 0.0f;
+    return g > 0.0f ? g : 0.0f;
+  } else {
+    const float z = ACT == kActSilu ? g : kGelu * (g + kGeluCube * g * g * g);
+    const float dz = ACT == kActSilu ? 1.0f : kGelu * (1.0f + 3.0f * kGeluCube * g * g);
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
+    const float both = s * (1.0f - s);
+    *slope = s + (both == 0.0f ? 0.0f : g * both * dz);  // far out dz may be infinite
+    return g * s;
+  }
+}
+
+// What the forward call keeps for the backward one: planes of 16 bits per unit and token.  h is rounded to bf16 as the second
+// product reads it.  g and u keep 24 bits of their fp32 (15 of the significand), the upper 16 in planes of their own and the
+// lower 8 of both in a third (GatedKept): rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to dwg instead
+// of 0.0024 (0.0017 is the rounding of dwg itself).
+__device__ __forceinline__ uint32_t upper_pair(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// The second bytes of a g pair and a u pair: g0 u0 g1 u1.
+__device__ __forceinline__ uint32_t lower_pair(float g0, float u0, float g1, float u1) {
+  const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(u0), __float_as_uint(g0), 0x0C0C0501u);
+  return a | __builtin_amdgcn_perm(__float_as_uint(u1), __float_as_uint(g1), 0x05010C0Cu);
+}
+__device__ __forceinline__ void unpack_kept(const uint4& g, const uint4& u, const uint4& low, float (&gv)[8], float (&uv)[8]) {
+  const uint32_t gd[4] = {g.x, g.y, g.z, g.w}, ud[4] = {u.x, u.y, u.z, u.w}, ld[4] = {low.x, low.y, low.z, low.w};
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {  // bytes 0 to 3 of a selector: the second operand's, 4 to 7: the first one's
+    gv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0504000Cu));
+    uv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0504010Cu));
+    gv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0706020Cu));
+    uv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0706030Cu));
+  }
+}
+
+// Calls f with the activation as a type.
+template <typename F>
+hipError_t with_activation(int act, F f) {
+  if (act == kActRelu) return f(std::integral_constant<int, kActRelu>{});
+  if (act == kActSilu) return f(std::integral_constant<int, kActSilu>{});
+  return f(std::integral_constant<int, kActGelu>{});
+}
+
+}  // namespace hire

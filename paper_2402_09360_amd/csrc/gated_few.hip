@@ -1,0 +1,408 @@
+// The dense gated FFN, forward, for up to 64 tokens: bound by reading the three matrices once (6 d d_ff bytes).  Tokens are the
+// small side of 16 x 16 x 32 matrix instructions, whose other operand comes straight from memory into registers.
+#include "gated.h"
+
+namespace hire {
+namespace {
+
+// ---- the first layer's products ------------------------------------------------------
+// g and u of RU times sixteen units for NT times sixteen tokens: one wave's part of k, in steps of 64 that the SLICES waves of a
+// workgroup take in turn.  A lane holds 32 bytes of one row of each matrix per step (k 64 s + 16 q ... of row lane % 16, q =
+// lane / 16) and of one token of each tile: which k meet in an instruction is the same for both, so any order of them will do.
+// Every workgroup starts at another step: rows are a power of two apart more often than not, and where all start with their first
+// columns the requests crowd on a few of the memory's channels (one token, d = 2048, 16384 units: 31.6 -> 24.7 us).
+template <int NT, int RU, int SLICES>
+__device__ __forceinline__ void up_products(const uint16_t* __restrict__ x, int T, const GatedLayer& L, int unit0, int slice,
+                                            f32x4v (&g)[RU][NT], f32x4v (&u)[RU][NT]) {
+  const int lane = lane_id(), q = lane >> 4, chunks = L.d / 8, steps = (chunks + 7) / 8;
+  const int turn = (int)((blockIdx.x * 5u) % (unsigned)steps);
+  const uint4 *pg[RU], *pu[RU], *px[NT];
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    const size_t row = (size_t)min(unit0 + 16 * r + (lane & 15), L.d_ff - 1) * L.d;
+    pg[r] = reinterpret_cast<const uint4*>(L.wg + row);
+    pu[r] = reinterpret_cast<const uint4*>(L.wu + row);
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) px[t] = reinterpret_cast<const uint4*>(x + (size_t)min(16 * t + (lane & 15), T - 1) * L.d);
+  auto chunk_of = [&](int s) { return 8 * (s + turn < steps ? s + turn : s + turn - steps) + 2 * q; };
+  auto load = [&](int s, uint4 (&wv)[RU][4], uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
+    const int c = chunk_of(s), a = min(c, chunks - 1), b = min(c + 1, chunks - 1);
+#pragma unroll
+    for (int r = 0; r < RU; ++r) wv[r][0] = pg[r][a], wv[r][1] = pg[r][b], wv[r][2] = pu[r][a], wv[r][3] = pu[r][b];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) xv[t][0] = px[t][a], xv[t][1] = px[t][b];
+  };
+  auto multiply = [&](int s, const uint4 (&wv)[RU][4], const uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
+    const int c = chunk_of(s);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t keep = c + e < chunks ? 0xFFFFFFFFu : 0u;  // behind the end of k both are zeros
+      auto masked = [&](const uint4& v) {
+        const uint4 m = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
+        bf16x8v b;
+        __builtin_memcpy(&b, &m, 16);
+        return b;
+      };
+      bf16x8v xf[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xf[t] = masked(xv[t][e]);
+#pragma unroll
+      for (int r = 0; r < RU; ++r) {
+        const bf16x8v wgv = masked(wv[r][e]), wuv = masked(wv[r][2 + e]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          g[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wgv, xf[t], g[r][t], 0, 0, 0);
+          u[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wuv, xf[t], u[r][t], 0, 0, 0);
+        }
+      }
+    }
+  };
+  uint4 wa[RU][4], xa[NT][2];
+  if constexpr (RU > 1) {  // the sums leave room for one step; the waves of a SIMD overlap theirs
+    for (int s = slice; s < steps; s += SLICES) {
+      load(s, wa, xa);
+      multiply(s, wa, xa);
+    }
+  } else {
+    uint4 wb[RU][4], xb[NT][2];
+    int s = slice;
+    if (s >= steps) return;
+    load(s, wa, xa);
+    for (; s + SLICES < steps; s += 2 * SLICES) {
+      load(s + SLICES, wb, xb);
+      multiply(s, wa, xa);
+      load(min(s + 2 * SLICES, steps - 1), wa, xa);  // not used where it repeats the last step
+      multiply(s + SLICES, wb, xb);
+    }
+    if (s < steps) multiply(s, wa, xa);
+  }
+}
+
+// Adds the slices' sums in their order; red: LDS, [groups of units][SLICES][2 NT 256].  unit (of the group's sixteen) and token
+// of value i; f(unit, token, g, u).
+template <int NT, int SLICES, typename F>
+__device__ __forceinline__ void join_slices(const float* red, int i, F f) {
+  const int unit = i & 15, token = i >> 4, at = (token >> 4) * 256 + ((unit >> 2) * 16 + (token & 15)) * 4 + (unit & 3);
+  float g = red[at], u = red[NT * 256 + at];
+#pragma unroll
+  for (int s = 1; s < SLICES; ++s) g += red[s * 2 * NT * 256 + at], u += red[(s * 2 + 1) * NT * 256 + at];
+  f(unit, token, g, u);
+}
+template <int NT>
+__device__ __forceinline__ void leave_slice(float* red, const f32x4v (&g)[NT], const f32x4v (&u)[NT]) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    *reinterpret_cast<f32x4v*>(red + (t * 64 + lane_id()) * 4) = g[t];
+    *reinterpret_cast<f32x4v*>(red + ((NT + t) * 64 + lane_id()) * 4) = u[t];
+  }
+}
+__device__ __forceinline__ void keep_gated(const GatedKept& kept, size_t at, float g, float u) {
+  kept.g[at] = (uint16_t)(__float_as_uint(g) >> 16);
+  kept.u[at] = (uint16_t)(__float_as_uint(u) >> 16);
+  kept.low[at] = (uint16_t)((__float_as_uint(g) >> 8 & 0xFFu) | (__float_as_uint(u) & 0xFF00u));
+}
+
+constexpr int kUpWaves = 4;
+
+template <int ACT, int NT, int RU>
+__global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const uint16_t* __restrict__ x, int T, GatedKept kept) {
+  __shared__ float red[kUpWaves * 2 * NT * 256];
+  const int unit0 = blockIdx.x * 16 * RU;
+  f32x4v g[RU][NT] = {}, u[RU][NT] = {};
+  up_products<NT, RU, kUpWaves>(x, T, L, unit0, wave_id(), g, u);
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    if (r > 0) __syncthreads();
+    leave_slice<NT>(red + wave_id() * 2 * NT * 256, g[r], u[r]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 256; i += 64 * kUpWaves)
+      join_slices<NT, kUpWaves>(red, i, [&](int unit, int token, float gv, float uv) {
+        const int f = unit0 + 16 * r + unit;
+        if (token >= T || f >= L.d_ff) return;
+        const size_t at = (size_t)token * L.d_ff + f;
+        float slope;
+        const __bf16 h = (__bf16)(activation<ACT>(gv, &slope) * uv);
+        __builtin_memcpy(kept.h + at, &h, 2);
+        if (kept.g) keep_gated(kept, at, gv, uv);
+      });
+  }
+}
+
+// ---- the second layer ---------------------------------------------------------------------
+// 32 rows by 128 columns of the matrix by NT tiles of tokens: lane l has eight columns (8 (l % 16) ...) of eight rows (8 (l / 16)
+// ...).  Column c of the eight, taken from all lanes, is one instruction's operand: its k are the rows, its columns 8 n + c.
+__device__ __forceinline__ bf16x8v column_of(const uint4 (&rows)[8], int c) {
+  uint32_t d[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const uint32_t lo[4] = {rows[2 * p].x, rows[2 * p].y, rows[2 * p].z, rows[2 * p].w};
+    const uint32_t hi[4] = {rows[2 * p + 1].x, rows[2 * p + 1].y, rows[2 * p + 1].z, rows[2 * p + 1].w};
+    d[p] = __builtin_amdgcn_perm(hi[c / 2], lo[c / 2], c % 2 ? 0x07060302u : 0x05040100u);
+  }
+  bf16x8v v;
+  __builtin_memcpy(&v, d, 16);
+  return v;
+}
+// Rows row0 + 8 (l / 16) ... of eight, as far as they lie in front of `end` (others: zeros, nothing of them is used).
+__device__ __forceinline__ void load_rows(const uint16_t* __restrict__ w, int d, int chunk, int row0, int end, uint4 (&rows)[8]) {
+  const int first = row0 + 8 * (lane_id() >> 4);
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+    rows[r] = load_streaming(reinterpret_cast<const uint4*>(w + (size_t)min(first + r, end - 1) * d) + chunk);
+}
+__device__ __forceinline__ void mask_rows(int row0, int end, uint4 (&rows)[8]) {
+  const int first = row0 + 8 * (lane_id() >> 4);
+#pragma unroll
+  for (int r = 0; r < 8; ++r)
+    if (first + r >= end) rows[r] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+constexpr int kDownWaves = 8;
+
+// Columns 128 blockIdx.x ..., rows of part blockIdx.y: the waves take blocks of 32 rows in turn.  The parts' sums are joined by
+// k_join_parts; one part only: y itself.
+template <int NT>
+__global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(const uint16_t* __restrict__ w2, const uint16_t* __restrict__ h, int T,
+                                                                int d, int d_ff, float* __restrict__ part,
+                                                                uint16_t* __restrict__ y) {
+  __shared__ float red[kDownWaves * 2048];
+  const int lane = lane_id(), wave = wave_id(), parts = gridDim.y, blocks = (d_ff + 31) / 32;
+  const int b0 = (int)((long long)blocks * blockIdx.y / parts), b1 = (int)((long long)blocks * (blockIdx.y + 1) / parts);
+  const int chunk = min((int)blockIdx.x * 16 + (lane & 15), d / 8 - 1);
+  const uint16_t* ph[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) ph[t] = h + (size_t)min(16 * t + (lane & 15), T - 1) * d_ff;
+  f32x4v acc[NT][8] = {};
+  auto load = [&](int b, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
+    load_rows(w2, d, chunk, 32 * b, d_ff, rows);
+    const int at = min(32 * b + 8 * (lane >> 4), d_ff - 8);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) hv[t] = *reinterpret_cast<const uint4*>(ph[t] + at);
+  };
+  auto multiply = [&](int b, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
+    if (32 * b + 32 > d_ff) {  // uniform; d_ff is a multiple of 8, so a lane's eight rows are there or not as a whole
+      mask_rows(32 * b, d_ff, rows);
+      if (32 * b + 8 * (lane >> 4) >= d_ff) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) hv[t] = make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+    bf16x8v hf[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) __builtin_memcpy(&hf[t], &hv[t], 16);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8v col = column_of(rows, c);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hf[t], col, acc[t][c], 0, 0, 0);
+    }
+  };
+  uint4 ra[8], ha[NT];
+  int b = b0 + wave;
+  if constexpr (NT > 2) {  // the sums take half of the registers: one block at a time
+    for (; b < b1; b += kDownWaves) {
+      load(b, ra, ha);
+      multiply(b, ra, ha);
+    }
+  } else if (b < b1) {
+    uint4 rb[8], hb[NT];
+    load(b, ra, ha);
+    for (; b + kDownWaves < b1; b += 2 * kDownWaves) {
+      load(b + kDownWaves, rb, hb);
+      multiply(b, ra, ha);
+      load(min(b + 2 * kDownWaves, blocks - 1), ra, ha);  // not used where it repeats the last block
+      multiply(b + kDownWaves, rb, hb);
+    }
+    if (b < b1) multiply(b, ra, ha);
+  }
+  // acc[t][c][i]: token 16 t + 4 (lane / 16) + i, column 8 (lane % 16) + c; a tile of tokens at a time through LDS
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t > 0) __syncthreads();
+    float* mine = red + wave * 2048;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < 8; c += 4)
+        *reinterpret_cast<float4*>(mine + (4 * (lane >> 4) + i) * 128 + 8 * (lane & 15) + c) =
+            make_float4(acc[t][c][i], acc[t][c + 1][i], acc[t][c + 2][i], acc[t][c + 3][i]);
+    __syncthreads();
+    const int token = 16 * t + (int)threadIdx.x / 32, col = blockIdx.x * 128 + (int)threadIdx.x % 32 * 4;
+    float4 s = reinterpret_cast<const float4*>(red)[threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < kDownWaves; ++w) {
+      const float4 v = reinterpret_cast<const float4*>(red + w * 2048)[threadIdx.x];
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    if (token < T && col < d) {
+      const size_t at = (size_t)token * d + col;
+      if (parts > 1) {
+        *reinterpret_cast<float4*>(part + (size_t)blockIdx.y * T * d + at) = s;
+      } else {
+        const float f[4] = {s.x, s.y, s.z, s.w};
+        *reinterpret_cast<uint2*>(y + at) = pack4(f);
+      }
+    }
+  }
+}
+
+// Parts of the second layer's rows: about 512 workgroups, of at least one block of 32 rows per wave.
+int down_parts(int d, int d_ff) {
+  const int columns = (d + 127) / 128, most = (d_ff + 32 * kDownWaves - 1) / (32 * kDownWaves);
+  int parts = 512 / columns;
+  parts = parts < 1 ? 1 : (parts > 16 ? 16 : parts);
+  return parts < most ? parts : most;
+}
+
+// ---- both layers in one kernel: the fewest tokens ---------------------------------------------
+// A workgroup takes 16 GROUPS units through both layers: their g and u, h through LDS, and the contribution of their
+// rows of the second matrix to y, whose loads go out before the waves join their sums.  The workgroups' parts of y, T d values
+// each, are added by k_join_units.
+template <int ACT, int GROUPS, int kOneWaves>
+__global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, const uint16_t* __restrict__ x, int T, GatedKept kept,
+                                                              float* __restrict__ part) {
+  constexpr int kSlices = kOneWaves / GROUPS, kUnits = 16 * GROUPS, kBlocks = (kUnits + 31) / 32;
+  __shared__ float red[kOneWaves * 512];
+  __shared__ __align__(16) __bf16 hidden[16 * kBlocks * 32];
+  const int lane = lane_id(), wave = wave_id(), unit0 = blockIdx.x * kUnits, end = min(unit0 + kUnits, L.d_ff);
+  const int group = wave % GROUPS, columns = (L.d + 127) / 128;
+  f32x4v g[1][1] = {}, u[1][1] = {};
+  up_products<1, 1, kSlices>(x, T, L, unit0 + 16 * group, wave / GROUPS, g, u);
+  auto chunk_of = [&](int block) { return min(16 * block + (lane & 15), L.d / 8 - 1); };
+  uint4 rows[kBlocks][8];
+#pragma unroll
+  for (int b = 0; b < kBlocks; ++b) load_rows(L.w2u, L.d, chunk_of(min(wave, columns - 1)), unit0 + 32 * b, end, rows[b]);
+  leave_slice<1>(red + (group * kSlices + wave / GROUPS) * 512, g[0], u[0]);
+  for (int i = threadIdx.x; i < 16 * kBlocks * 32; i += 64 * kOneWaves) hidden[i] = (__bf16)0.0f;
+  __syncthreads();
+  for (int i = threadIdx.x; i < GROUPS * 256; i += 64 * kOneWaves)
+    join_slices<1, kSlices>(red + i / 256 * kSlices * 512, i % 256, [&](int unit, int token, float gv, float uv) {
+      const int in = i / 256 * 16 + unit;
+      if (token >= T || unit0 + in >= L.d_ff) return;
+      float slope;
+      const __bf16 h = (__bf16)(activation<ACT>(gv, &slope) * uv);
+      hidden[token * kBlocks * 32 + in] = h;
+      if (kept.g) {
+        const size_t at = (size_t)token * L.d_ff + unit0 + in;
+        __builtin_memcpy(kept.h + at, &h, 2);
+        keep_gated(kept, at, gv, uv);
+      }
+    });
+  __syncthreads();
+  for (int block = wave; block < columns; block += kOneWaves) {
+    f32x4v acc[8] = {};
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      if (unit0 + 32 * b + 32 > end) mask_rows(unit0 + 32 * b, end, rows[b]);
+      const bf16x8v hf = *reinterpret_cast<const bf16x8v*>(hidden + ((lane & 15) * kBlocks + b) * 32 + 8 * (lane >> 4));
+#pragma unroll
+      for (int c = 0; c < 8; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hf, column_of(rows[b], c), acc[c], 0, 0, 0);
+      if (block + kOneWaves < columns) load_rows(L.w2u, L.d, chunk_of(block + kOneWaves), unit0 + 32 * b, end, rows[b]);
+    }
+    const int col = 128 * block + 8 * (lane & 15);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int token = 4 * (lane >> 4) + i;
+      if (token < T && col < L.d) {
+        float4* to = reinterpret_cast<float4*>(part + ((size_t)blockIdx.x * T + token) * L.d + col);
+        to[0] = make_float4(acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
+        to[1] = make_float4(acc[4][i], acc[5][i], acc[6][i], acc[7][i]);
+      }
+    }
+  }
+}
+
+// Sum of many parts of few values: sixteen threads share four values, each adds every sixteenth part.
+__global__ __launch_bounds__(256) void k_join_units(const float* __restrict__ part, uint16_t* __restrict__ y, int parts, int quads) {
+  __shared__ float4 sums[256];
+  const int quad = blockIdx.x * 16 + (int)threadIdx.x % 16, at = min(quad, quads - 1);
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+  for (int r = (int)threadIdx.x / 16; r < parts; r += 16) {
+    const float4 v = reinterpret_cast<const float4*>(part)[(size_t)r * quads + at];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  sums[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x >= 16 || quad >= quads) return;
+  for (int r = 1; r < 16; ++r) {
+    const float4 v = sums[16 * r + threadIdx.x];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  }
+  const float f[4] = {s.x, s.y, s.z, s.w};
+  reinterpret_cast<uint2*>(y)[quad] = pack4(f);
+}
+
+// Sixteens of units of a workgroup: a workgroup for every compute unit, but no more than are resident at once.  d = 2048, one
+// token, us with 1 / 2 / 4 of them: 5000 units 26.5 / 18.7 / -, 9000 - / 33.3 / 31.0, 16384 - / 41.7 / 38.3.
+int one_groups(int d_ff) {
+  const int groups = (d_ff + 15) / 16;
+  return groups > 512 ? 4 : (groups > 256 ? 2 : 1);
+}
+int one_parts(int d_ff) { return (d_ff + 16 * one_groups(d_ff) - 1) / (16 * one_groups(d_ff)); }
+// One kernel and the join of its parts is shorter than two and a join as long as the parts' way through memory is: up to 35 MB
+// there and back.  us, one kernel / two: d = 2048, 16384 units, one token 38.3 / 47.3, eight (34 MB) 43.2 / 50.0, sixteen 51.4
+// / 51.9; d = 4096, 8192 units, four (34 MB) 47.9 / 49.0, eight 54.5 / 50.4; d = 8192, 28000 units, one (29 MB) 249 / 260, four
+// 278 / 264; d = 256, 1024 units, one 7.2 / 9.4.
+bool one_kernel(int T, int d, int d_ff) { return T <= 16 && (long long)one_parts(d_ff) * T * d * 8 <= (35ll << 20); }
+
+template <int GROUPS, int kOneWaves>
+hipError_t launch_one(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
+  const int parts = one_parts(L.d_ff), quads = T * L.d / 4;
+  const hipError_t e = with_activation(L.act, [&](auto act) {
+    return launch(&k_gated_one<decltype(act)::value, GROUPS, kOneWaves>, dim3((unsigned)parts), dim3(64 * kOneWaves), 0, s, L, x, T, kept, part);
+  });
+  return e != hipSuccess ? e
+                         : launch(&k_join_units, dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, part, y, parts, quads);
+}
+
+template <int NT, int RU>
+hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
+  hipError_t e = with_activation(L.act, [&](auto act) {
+    return launch(&k_gated_up<decltype(act)::value, NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
+                  dim3(64 * kUpWaves), 0, s, L, x, T, kept);
+  });
+  if (e != hipSuccess) return e;
+  const int parts = down_parts(L.d, L.d_ff);
+  e = launch(&k_gated_down<NT>, dim3((unsigned)((L.d + 127) / 128), (unsigned)parts), dim3(64 * kDownWaves), 0, s, L.w2u, kept.h, T,
+             L.d, L.d_ff, part, y);
+  if (e != hipSuccess || parts == 1) return e;
+  return launch_join_parts(part, y, true, parts, (long long)T * L.d, s);
+}
+
+// Units of a workgroup of the first layer, in sixteens.  More of them share what is read of the tokens, which comes from the L2
+// for every workgroup; but 256 workgroups should be left.
+template <int NT, int WIDEST>
+hipError_t launch_few_by_width(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
+                               hipStream_t s) {
+  const int groups = (L.d_ff + 15) / 16;
+  if constexpr (WIDEST >= 4)
+    if (groups >= 4 * 256) return launch_few<NT, 4>(L, x, T, y, kept, part, s);
+  if (groups >= 2 * 256) return launch_few<NT, 2>(L, x, T, y, kept, part, s);
+  return launch_few<NT, 1>(L, x, T, y, kept, part, s);
+}
+
+}  // namespace
+
+size_t gated_few_part_bytes(int T, int d, int d_ff) {
+  if (one_kernel(T, d, d_ff)) return (size_t)one_parts(d_ff) * T * d * sizeof(float);
+  const int parts = down_parts(d, d_ff);
+  return parts > 1 ? (size_t)parts * T * d * sizeof(float) : 0;
+}
+
+hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
+                            hipStream_t s) {
+  if (one_kernel(T, L.d, L.d_ff)) {
+    const int groups = one_groups(L.d_ff);
+    if (groups == 4) return launch_one<4, 8>(L, x, T, y, kept, part, s);
+    return groups == 2 ? launch_one<2, 8>(L, x, T, y, kept, part, s) : launch_one<1, 16>(L, x, T, y, kept, part, s);
+  }
+  const int tiles = (T + 15) / 16;
+  if (tiles == 1) return launch_few_by_width<1, 2>(L, x, T, y, kept, part, s);
+  if (tiles == 2) return launch_few_by_width<2, 2>(L, x, T, y, kept, part, s);
+  if (tiles == 3) return launch_few_by_width<3, 4>(L, x, T, y, kept, part, s);
+  return launch_few_by_width<4, 4>(L, x, T, y, kept, part, s);
+}
+
+}  // namespace hire

@@ -1,27 +1,8 @@
 // The dense gated FFN, forward and backward, for any number of tokens.
-#include "dense_epilogue.h"
-#include "kernels.h"
+#include "gated.h"
 
 namespace hire {
 namespace {
-
-// Activation a(g) and its derivative.  silu and the tanh form of gelu are both g s(z) with the logistic function s:
-// z = g, or 2 sqrt(2/pi) (g + 0.044715 g^3).  a' = s + g s (1 - s) z'.
-constexpr float kGelu = 1.5957691216057308f, kGeluCube = 0.044715f, kLog2E = 1.4426950408889634f;
-template <int ACT>
-__device__ __forceinline__ float activation(float g, float* slope) {
-  if constexpr (ACT == kActRelu) {
-    *slope = g > 0.0f ? 1.0f : 0.0f;
-    return g > 0.0f ? g : 0.0f;
-  } else {
-    const float z = ACT == kActSilu ? g : kGelu * (g + kGeluCube * g * g * g);
-    const float dz = ACT == kActSilu ? 1.0f : kGelu * (1.0f + 3.0f * kGeluCube * g * g);
-    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2E * z));
-    const float both = s * (1.0f - s);
-    *slope = s + (both == 0.0f ? 0.0f : g * both * dz);  // far out dz may be infinite
-    return g * s;
-  }
-}
 
 struct StoreBf16 {
   uint16_t* c[3];
@@ -34,36 +15,10 @@ struct StoreBf16 {
   }
 };
 
-// What the forward call keeps for the backward one: planes of 16 bits per unit and token.  h is rounded to bf16 as the second
-// product reads it.  g and u keep 24 bits of their fp32 (15 of the significand), the upper 16 in planes of their own and the
-// lower 8 of both in a third: rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to dwg instead
-// of 0.0024 (0.0017 is the rounding of dwg itself).
-struct KeptPlanes {
-  uint16_t *h, *g, *u, *low;
-};
-__device__ __forceinline__ uint32_t upper_pair(float a, float b) {
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-}
-// The second bytes of a g pair and a u pair: g0 u0 g1 u1.
-__device__ __forceinline__ uint32_t lower_pair(float g0, float u0, float g1, float u1) {
-  const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(u0), __float_as_uint(g0), 0x0C0C0501u);
-  return a | __builtin_amdgcn_perm(__float_as_uint(u1), __float_as_uint(g1), 0x05010C0Cu);
-}
-__device__ __forceinline__ void unpack_kept(const uint4& g, const uint4& u, const uint4& low, float (&gv)[8], float (&uv)[8]) {
-  const uint32_t gd[4] = {g.x, g.y, g.z, g.w}, ud[4] = {u.x, u.y, u.z, u.w}, ld[4] = {low.x, low.y, low.z, low.w};
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {  // bytes 0 to 3 of a selector: the second operand's, 4 to 7: the first one's
-    gv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0504000Cu));
-    uv[2 * q] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0504010Cu));
-    gv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(gd[q], ld[q], 0x0706020Cu));
-    uv[2 * q + 1] = __uint_as_float(__builtin_amdgcn_perm(ud[q], ld[q], 0x0706030Cu));
-  }
-}
-
 // h = a(g) u.
 template <int ACT>
 struct StoreGated {
-  KeptPlanes kept;  // g null: h only
+  GatedKept kept;  // g null: h only
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
     for_rows<true>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[2][8]) {
@@ -91,7 +46,7 @@ struct StoreGated {
 // The sums are dh: dg = dh u a'(g), du = dh a(g), rounded to bf16 for the products that follow.
 template <int ACT>
 struct StoreGateSlopes {
-  KeptPlanes kept;
+  GatedKept kept;
   uint16_t *dg, *du;
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
@@ -123,32 +78,23 @@ hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStrea
   return e != hipSuccess ? e : launch_join_parts(part, out, true, g.splits, (long long)g.M * g.N, s);
 }
 
-template <typename F>
-hipError_t with_activation(int act, F f) {
-  if (act == kActRelu) return f(std::integral_constant<int, kActRelu>{});
-  if (act == kActSilu) return f(std::integral_constant<int, kActSilu>{});
-  return f(std::integral_constant<int, kActGelu>{});
-}
-
 }  // namespace
 
 size_t gated_part_bytes(int T, int d, int d_ff, int segments) {
+  if (segments == 1 && T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff);
   const int s = product_splits(T, d, segments * ((d_ff + kGemmStep - 1) / kGemmStep));
   return s > 1 ? (size_t)s * T * d * sizeof(float) : 0;
 }
 
-namespace {
-KeptPlanes planes_of(const GatedKept& k) { return KeptPlanes{k.h, k.g, k.u, k.low}; }
-}  // namespace
-
 hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                                 hipStream_t s) {
+  if (T <= kGatedFewTokens) return launch_gated_few(L, x, T, y, kept, part, s);
   GemmArgs up{};
   up.a[0] = x, up.b[0] = L.wg, up.b[1] = L.wu;
   up.M = T, up.N = L.d_ff, up.K = L.d, up.lda = up.ldb = 2u * L.d;
   up.segments = up.products = up.splits = 1;
   const hipError_t e = with_activation(L.act, [&](auto act) {
-    return launch_product<true, true, true, false>(up, StoreGated<decltype(act)::value>{planes_of(kept)}, s);
+    return launch_product<true, true, true, false>(up, StoreGated<decltype(act)::value>{kept}, s);
   });
   if (e != hipSuccess) return e;
   GemmArgs down{};
@@ -168,7 +114,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
     a.segments = a.products = a.splits = 1;
     e = with_activation(L.act, [&](auto act) {
-      return launch_product<true, true, false, false>(a, StoreGateSlopes<decltype(act)::value>{planes_of(kept), dg, du}, s);
+      return launch_product<true, true, false, false>(a, StoreGateSlopes<decltype(act)::value>{kept, dg, du}, s);
     });
     if (e != hipSuccess) return e;
   }

@@ -479,7 +479,7 @@ struct GatedLayer {
   const uint16_t* wu;
   const uint16_t* w2u;
 };
-// Bytes of the fp32 parts of a product with a T x d result and k = segments * d_ff (0: it is not split).
+// Bytes of the fp32 parts of the forward pass's second product (segments 1) or of dx (2); 0: it is not split.
 size_t gated_part_bytes(int T, int d, int d_ff, int segments);
 // Planes [T, d_ff] of 16 bits that the forward pass leaves for the backward pass; g, u, low null: h only.
 struct GatedKept {
@@ -491,6 +491,12 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
 hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
                                  uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
                                  float* part, hipStream_t s);
+
+// ---- gated_few.hip: the forward pass of up to kGatedFewTokens tokens
+constexpr int kGatedFewTokens = 64;
+size_t gated_few_part_bytes(int T, int d, int d_ff);
+hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
+                            hipStream_t s);
 
 // ---- mxfp4.hip: microscaled 4-bit floating point ---------------------------------
 hipError_t launch_pack_mxfp4(const uint16_t* w, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s);
