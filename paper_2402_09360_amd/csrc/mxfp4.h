@@ -10,9 +10,13 @@ typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 
 constexpr int kMxBlock = 32;
 
-// 2^(byte - 127) as fp32 (byte 0: the subnormal 2^-127; 255: NaN).
-__device__ __forceinline__ float mx_scale(uint32_t byte) {
-  return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7FC00000u : byte << 23);
+// A scale byte as the conversions take it: in the exponent of an fp32.  They read nothing else of it, so that byte 0 is 2^-127
+// and 255 makes NaN of every code.
+__device__ __forceinline__ float mx_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+// The same of byte J of a word.
+template <int J>
+__device__ __forceinline__ float mx_scale_of(uint32_t word) {
+  return __uint_as_float((J == 3 ? word >> 1 : word << (23 - 8 * J)) & 0x7F800000u);
 }
 
 // Eight codes (one dword) times a scale as bf16 pairs: exact (two bits of significand) but for magnitudes beyond the type's

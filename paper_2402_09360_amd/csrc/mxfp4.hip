@@ -52,16 +52,63 @@ __global__ __launch_bounds__(256) void k_unpack_mxfp4(const uint32_t* __restrict
 }
 
 // ---- few tokens -----------------------------------------------------------------
-// A wave multiplies RU times sixteen rows with NT times sixteen tokens; the waves of a workgroup take the steps of 128 columns
-// in turn and their sums are added in LDS in a fixed order.  A lane holds one block (32 codes) of one row per step.
-constexpr int kFewWaves = 4;
+// A wave multiplies RU times sixteen rows with NT times sixteen tokens in steps of 128 columns, four blocks; the WAVES waves of a
+// workgroup take the steps in turn, and their sums are added in LDS in a fixed order.  A lane gets one block (sixteen bytes) of
+// one row: block q = lane / 16 of row lane % 16.
+//   Packed tokens: the same of a token, and one scaled instruction for the four blocks.
+//   bf16 tokens: one instruction per block, whose lane holds columns 8 q ... of the block; so the four lanes of a row first
+// exchange words, after which word q of block j is word j of lane q.  Then sixteen bytes of a token are 64 in a row of four
+// lanes; of a lane's own block they would be 16 bytes every 64.
+template <int RU>
+__device__ __forceinline__ void exchange_blocks(uint4 (&c)[RU]) {
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    const auto a = __builtin_amdgcn_permlane32_swap(c[r].x, c[r].z, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(c[r].y, c[r].w, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    c[r] = make_uint4(lo[0], lo[1], hi[0], hi[1]);
+  }
+}
+// The four scale bytes of blocks 4 s ... of a row; behind the last one: 127 (the codes there are zeros).
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* row, int s, int blocks, bool words) {
+  if (words) return reinterpret_cast<const uint32_t*>(row)[s];
+  uint32_t v = 0u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v |= (4 * s + e < blocks ? (uint32_t)row[min(4 * s + e, blocks - 1)] : 127u) << (8 * e);
+  return v;
+}
 
-template <bool PACKED_TOKENS, int NT, int RU>
-__global__ __launch_bounds__(64 * kFewWaves) void k_mx_few(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                           const void* __restrict__ x, const uint8_t* __restrict__ x_scales,
-                                                           int T, int rows, int cols, void* __restrict__ y, int y_bf16) {
-  __shared__ float sums[kFewWaves][RU * NT * 256];
-  const int lane = lane_id(), wave = wave_id(), kq = lane >> 4, blocks = cols / kMxBlock;
+// The words of TURN neighbouring steps, s0 a multiple of TURN: one load, in which neighbouring lanes of a row take neighbouring
+// words, so that a line of scale bytes is asked for once for all of them and not for every step again.
+template <int TURN>
+__device__ __forceinline__ uint32_t scale_words(const uint8_t* row, int s0, int blocks, bool words) {
+  const int s = s0 + ((lane_id() >> 4) & (TURN - 1));
+  return scale_word(row, min(s, (blocks - 1) / 4), blocks, words);
+}
+template <int TURN>
+__device__ __forceinline__ void spread_words(uint32_t mine, uint32_t (&word)[TURN]) {
+  static_assert(TURN == 1 || TURN == 2 || TURN == 4, "lanes of a row");
+  if constexpr (TURN == 1) {
+    word[0] = mine;
+  } else if constexpr (TURN == 2) {
+    const auto w = __builtin_amdgcn_permlane16_swap(mine, mine, false, false);
+    word[0] = w[0], word[1] = w[1];
+  } else {
+    const auto h = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);
+    word[0] = lo[0], word[1] = lo[1], word[2] = hi[0], word[3] = hi[1];
+  }
+}
+
+template <bool PACKED_TOKENS, int NT, int RU, int WAVES, int TURN>
+__global__ __launch_bounds__(64 * WAVES) void k_mx_few(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                       const void* __restrict__ x, const uint8_t* __restrict__ x_scales, int T,
+                                                       int rows, int cols, int words, void* __restrict__ y, int y_bf16,
+                                                       float* __restrict__ part) {
+  __shared__ float sums[WAVES][RU * NT * 256];
+  const int lane = lane_id(), wave = wave_id(), q = lane >> 4, blocks = cols / kMxBlock;
   const int row0 = blockIdx.x * 16 * RU;
   const uint8_t *row[RU], *row_scale[RU];
 #pragma unroll
@@ -75,29 +122,26 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx_few(const uint8_t* __rest
   for (int t = 0; t < NT; ++t) token[t] = (size_t)min(16 * t + (lane & 15), T - 1);
 
   f32x4v acc[RU][NT] = {};
-  const int steps = (blocks + 3) / 4;
-  for (int s = wave; s < steps; s += kFewWaves) {
-    const int block = 4 * s + kq;
-    const bool there = block < blocks;
-    const int b = there ? block : blocks - 1;
+  const int turns = (blocks + 4 * TURN - 1) / (4 * TURN), steps = (blocks + 3) / 4;
+  const int first = (int)((long long)turns * blockIdx.y / gridDim.y), last = (int)((long long)turns * (blockIdx.y + 1) / gridDim.y);
+  const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
+  auto step = [&](int s, const uint32_t (&sc)[RU]) __attribute__((always_inline)) {
+    const bool there = 4 * s + q < blocks;
+    const int b = there ? 4 * s + q : blocks - 1;
     uint4 c[RU];
-    uint32_t sc[RU];
 #pragma unroll
-    for (int r = 0; r < RU; ++r) {
-      c[r] = load_streaming(reinterpret_cast<const uint4*>(row[r]) + b);
-      sc[r] = row_scale[r][b];
-    }
+    for (int r = 0; r < RU; ++r) c[r] = reinterpret_cast<const uint4*>(row[r])[b];
     if constexpr (PACKED_TOKENS) {
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         uint4 xc = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(x) + token[t] * (cols / 2))[b];
         const uint32_t xs = there ? x_scales[token[t] * blocks + b] : 127u;
-        if (!there) xc = make_uint4(0u, 0u, 0u, 0u);
+        if (!there) xc = zeros;
         const i32x8v xv = {(int)xc.x, (int)xc.y, (int)xc.z, (int)xc.w, 0, 0, 0, 0};
 #pragma unroll
         for (int r = 0; r < RU; ++r) {
           const i32x8v cv = {(int)c[r].x, (int)c[r].y, (int)c[r].z, (int)c[r].w, 0, 0, 0, 0};
-          acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(cv, xv, acc[r][t], 4, 4, 0, there ? (int)sc[r] : 127, 0,
+          acc[r][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(cv, xv, acc[r][t], 4, 4, 0, (int)(sc[r] >> (8 * q)), 0,
                                                                        (int)xs);
         }
       }
@@ -105,27 +149,54 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx_few(const uint8_t* __rest
       uint4 xv[NT][4];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + token[t] * cols) + 4 * b;
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + token[t] * cols) + q;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) xv[t][j] = there ? p[j] : make_uint4(0u, 0u, 0u, 0u);
+        for (int j = 0; j < 4; ++j) xv[t][j] = p[4 * min(4 * s + j, blocks - 1)];
       }
+      if (4 * s + 4 > blocks) {  // uniform: the last blocks are not there
+#pragma unroll
+        for (int r = 0; r < RU; ++r)
+          if (!there) c[r] = zeros;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (4 * s + j >= blocks) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) xv[t][j] = zeros;
+          }
+      }
+      exchange_blocks<RU>(c);
 #pragma unroll
       for (int r = 0; r < RU; ++r) {
-        const float scale = mx_scale(there ? sc[r] : 127u);
-        const uint32_t cd[4] = {c[r].x, c[r].y, c[r].z, c[r].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint4 w4 = mx_to_bf16(there ? cd[j] : 0u, scale);
+        auto block = [&](auto which, uint32_t code) {
+          constexpr int J = decltype(which)::value;
+          const uint4 w4 = mx_to_bf16(code, mx_scale_of<J>(sc[r]));
           bf16x8v wv;
           __builtin_memcpy(&wv, &w4, 16);
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             bf16x8v xf;
-            __builtin_memcpy(&xf, &xv[t][j], 16);
+            __builtin_memcpy(&xf, &xv[t][J], 16);
             acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xf, acc[r][t], 0, 0, 0);
           }
-        }
+        };
+        block(std::integral_constant<int, 0>{}, c[r].x);
+        block(std::integral_constant<int, 1>{}, c[r].y);
+        block(std::integral_constant<int, 2>{}, c[r].z);
+        block(std::integral_constant<int, 3>{}, c[r].w);
       }
+    }
+  };
+  for (int turn = first + wave; turn < last; turn += WAVES) {
+    uint32_t word[RU][TURN];
+#pragma unroll
+    for (int r = 0; r < RU; ++r) spread_words<TURN>(scale_words<TURN>(row_scale[r], turn * TURN, blocks, words), word[r]);
+#pragma unroll
+    for (int u = 0; u < TURN; ++u) {
+      if (TURN > 1 && turn * TURN + u >= steps) break;
+      uint32_t sc[RU];
+#pragma unroll
+      for (int r = 0; r < RU; ++r) sc[r] = word[r][u];
+      step(turn * TURN + u, sc);
     }
   }
   // acc[r][t]: token 16 t + lane % 16, rows 16 r + 4 (lane / 16) ... of this wave's columns
@@ -135,20 +206,260 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_mx_few(const uint8_t* __rest
     for (int t = 0; t < NT; ++t)
       *reinterpret_cast<f32x4v*>(&sums[wave][((r * NT + t) * 64 + lane) * 4]) = acc[r][t];
   __syncthreads();
-  for (int i = threadIdx.x; i < RU * NT * 256; i += 64 * kFewWaves) {
+  const bool parts = gridDim.y > 1;
+  float* out = parts ? part + (size_t)blockIdx.y * T * rows : static_cast<float*>(y);
+  for (int i = threadIdx.x; i < RU * NT * 256; i += 64 * WAVES) {
     // neighbouring threads: neighbouring rows of one token
     const int n = i % (16 * RU), tok = i / (16 * RU), at = ((n / 16 * NT + tok / 16) * 64 + (n % 16 / 4) * 16 + tok % 16) * 4 + n % 4;
     float v = sums[0][at];
 #pragma unroll
-    for (int q = 1; q < kFewWaves; ++q) v += sums[q][at];
+    for (int w = 1; w < WAVES; ++w) v += sums[w][at];
     if (tok < T && row0 + n < rows) {
       const size_t o = (size_t)tok * rows + row0 + n;
-      if (y_bf16)
+      if (y_bf16 && !parts)
         static_cast<__bf16*>(y)[o] = (__bf16)v;
       else
-        static_cast<float*>(y)[o] = v;
+        out[o] = v;
     }
   }
+}
+
+// ---- one bf16 token ---------------------------------------------------------------------
+// Whole rows by vector instructions: LPR lanes of a wave share a row, a lane has one block of it and the token's 32 values that go
+// with it, in registers for as long as the wave lives; so a wave's loads are whole rows without gaps, which the matrix
+// instructions' layout (64 bytes of sixteen rows) does not give.  SPAN waves share rows of more than 2048 columns.  A wave has the
+// kOneRows groups of rows that it works on and the next ones in flight.  256000 rows of 2048 columns: 50 us (5.6 TB/s; by matrix
+// instructions 66), 16384 rows 6.5 (7.3).  Two tokens this way take as long as by matrix instructions, 68 us: the additions.
+constexpr int kOneRows = 4;
+
+template <int LPR, int SPAN>
+__global__ __launch_bounds__(64 * SPAN) void k_mx_one(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                      const uint16_t* __restrict__ x, int rows, int cols, void* __restrict__ y,
+                                                      int y_bf16) {
+  constexpr int kRows = kWave / LPR, kBatch = kRows * kOneRows;
+  __shared__ float join[SPAN > 1 ? 2 * SPAN * kBatch : 1];
+  const int lane = lane_id(), wave = SPAN > 1 ? wave_id() : 0, blocks = cols / kMxBlock;
+  const int block = wave * LPR + lane % LPR, at = min(block, blocks - 1);
+  const bool there = block < blocks;
+  float xv[32];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    uint4 v = reinterpret_cast<const uint4*>(x + (size_t)at * 32)[p];
+    if (!there) v = make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) xv[8 * p + 2 * e] = bf16_lo(d[e]), xv[8 * p + 2 * e + 1] = bf16_hi(d[e]);
+  }
+  const int stride = gridDim.x * kBatch;
+  uint4 next[kOneRows];
+  uint32_t next_scale[kOneRows];
+  auto request = [&](int row0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kOneRows; ++u) {
+      const size_t row = (size_t)min(row0 + u * kRows + lane / LPR, rows - 1);
+      next[u] = load_streaming(reinterpret_cast<const uint4*>(codes + row * (cols / 2)) + at);
+      next_scale[u] = scales[row * blocks + at];
+    }
+  };
+  int turn = 0;
+  request(blockIdx.x * kBatch);
+  for (int row0 = blockIdx.x * kBatch; row0 < rows; row0 += stride, turn ^= 1) {
+    uint4 code[kOneRows];
+    uint32_t sc[kOneRows];
+#pragma unroll
+    for (int u = 0; u < kOneRows; ++u) code[u] = next[u], sc[u] = next_scale[u];
+    request(min(row0 + stride, rows - 1));  // not used behind the last row
+    float mine = 0.0f;  // lane u kRows + r of the first kBatch: that row's sum
+#pragma unroll
+    for (int u = 0; u < kOneRows; ++u) {
+      const float scale = mx_scale(there ? sc[u] : 127u);
+      const uint32_t d[4] = {code[u].x, code[u].y, code[u].z, code[u].w};
+      float s = 0.0f;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t word = there ? d[p] : 0u;
+        float w[8];
+        auto pair = [&](auto which) {
+          constexpr int P = decltype(which)::value;
+          const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, P);
+          w[2 * P] = v[0], w[2 * P + 1] = v[1];
+        };
+        pair(std::integral_constant<int, 0>{});
+        pair(std::integral_constant<int, 1>{});
+        pair(std::integral_constant<int, 2>{});
+        pair(std::integral_constant<int, 3>{});
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(w[e], xv[8 * p + e], s);
+      }
+      // the sum of the row's lanes, in its last one
+      s += dpp_move<0x111, 0xF>(0.0f, s);
+      s += dpp_move<0x112, 0xF>(0.0f, s);
+      s += dpp_move<0x114, 0xF>(0.0f, s);
+      if constexpr (LPR >= 16) s += dpp_move<0x118, 0xF>(0.0f, s);
+      if constexpr (LPR >= 32) s += dpp_move<0x142, 0xA>(0.0f, s);
+      if constexpr (LPR >= 64) s += dpp_move<0x143, 0xC>(0.0f, s);
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        const float sum = read_lane(s, r * LPR + LPR - 1);
+        if (lane == u * kRows + r) mine = sum;
+      }
+    }
+    if constexpr (SPAN > 1) {
+      float* place = join + turn * SPAN * kBatch;
+      if (lane < kBatch) place[wave * kBatch + lane] = mine;
+      lds_barrier();
+      if (wave == 0 && lane < kBatch)
+        for (int w = 1; w < SPAN; ++w) mine += place[w * kBatch + lane];
+    }
+    if (wave == 0 && lane < kBatch && row0 + lane < rows) {
+      if (y_bf16)
+        static_cast<__bf16*>(y)[row0 + lane] = (__bf16)mine;
+      else
+        static_cast<float*>(y)[row0 + lane] = mine;
+    }
+  }
+}
+
+// ---- few bf16 tokens, the tokens shared in LDS -----------------------------------------
+// RW waves of a workgroup have RU times sixteen rows each, all of them the same columns, and KW such groups of waves share the
+// four-block steps of a chunk of 256 columns; the tokens' chunk is in LDS, so what comes from the L2 for the tokens is shared by 16 RU RW
+// rows.  The next chunk's tokens and the wave's own codes of it are on their way while one is multiplied.
+// x in LDS: [16 NT tokens][512 bytes], 16-byte piece c of token t at c ^ (t % 16).
+constexpr int kSharedChunk = 256;
+constexpr int kSharedSteps = kSharedChunk / 128;
+
+template <int NT, int RU, int RW, int KW>
+__global__ __launch_bounds__(64 * RW * KW) void k_mx_shared(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                                            const uint16_t* __restrict__ x, int T, int rows, int cols, int words,
+                                                            void* __restrict__ y, int y_bf16) {
+  constexpr int kWaves = RW * KW, kSteps = kSharedSteps / KW, kPlace = 16 * NT * kSharedChunk * 2, kLoads = kPlace / 1024 / kWaves;
+  static_assert(KW <= 2 && kLoads * kWaves * 1024 == kPlace, "whole loads");
+  constexpr int kJoin = KW > 1 ? RW * RU * NT * 1024 : 0;
+  __shared__ __align__(1024) char smem[2 * kPlace > kJoin ? 2 * kPlace : kJoin];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), q = lane >> 4, blocks = cols / kMxBlock;
+  const int kw = wave % KW, row0 = (blockIdx.x * RW + wave / KW) * 16 * RU;
+  const uint8_t *row[RU], *row_scale[RU];
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    const int at = min(row0 + 16 * r + (lane & 15), rows - 1);
+    row[r] = codes + (size_t)at * (cols / 2);
+    row_scale[r] = scales + (size_t)at * blocks;
+  }
+  const int chunks = (cols + kSharedChunk - 1) / kSharedChunk;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
+  auto request_tokens = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      constexpr int kLanes = kSharedChunk / 8;  // of a token
+      const int piece = i * kWaves + wave, t = (piece * 64 + lane) / kLanes;
+      const int at = c * kSharedChunk + ((lane & (kLanes - 1)) ^ (t & 15)) * 8;
+      const void* from = x + (size_t)min(t, T - 1) * cols + at;
+      gemm_load_at(at < cols ? from : (const void*)kGemmZeros, lds0 + (uint32_t)(c & 1) * kPlace + piece * 1024);
+    }
+  };
+  uint4 next[kSteps][RU];
+  uint32_t next_scale[RU];  // of all steps of the chunk, as scale_words has them
+  auto request_codes = [&](int c) {
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      const int s = kSharedSteps * c + kw * kSteps + u, b = min(4 * s + q, blocks - 1);
+#pragma unroll
+      for (int r = 0; r < RU; ++r) {
+        next[u][r] = reinterpret_cast<const uint4*>(row[r])[b];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RU; ++r) next_scale[r] = scale_words<kSteps>(row_scale[r], kSharedSteps * c + kw * kSteps, blocks, words);
+  };
+  f32x4v acc[RU][NT] = {};
+  request_codes(0);
+  request_tokens(0);
+  for (int c = 0; c < chunks; ++c) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    uint4 code[kSteps][RU];
+    uint32_t sc[RU][kSteps];
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+      for (int r = 0; r < RU; ++r) {
+        // in registers before the next requests go out: behind them the compiler would wait for those too
+        asm volatile("" : "+v"(next[u][r].x), "+v"(next[u][r].y), "+v"(next[u][r].z), "+v"(next[u][r].w), "+v"(next_scale[r]));
+        code[u][r] = next[u][r];
+        if ((kSharedSteps * c + kw * kSteps + u) * 4 + q >= blocks) code[u][r] = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+    for (int r = 0; r < RU; ++r) spread_words<kSteps>(next_scale[r], sc[r]);
+    if (c + 1 < chunks) {
+      request_codes(c + 1);
+      request_tokens(c + 1);
+    }
+    const char* place = smem + (c & 1) * kPlace;
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      exchange_blocks<RU>(code[u]);
+      const int step = kw * kSteps + u;
+      auto block = [&](auto which) {
+        constexpr int J = decltype(which)::value;
+        bf16x8v xf[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+          xf[t] = *reinterpret_cast<const bf16x8v*>(place + (16 * t + (lane & 15)) * (2 * kSharedChunk) +
+                                                    ((((4 * step + J) * 4 + q) ^ (lane & 15)) << 4));
+#pragma unroll
+        for (int r = 0; r < RU; ++r) {
+          const uint32_t word = J == 0 ? code[u][r].x : (J == 1 ? code[u][r].y : (J == 2 ? code[u][r].z : code[u][r].w));
+          const uint4 w4 = mx_to_bf16(word, mx_scale_of<J>(sc[r][u]));
+          bf16x8v wv;
+          __builtin_memcpy(&wv, &w4, 16);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xf[t], acc[r][t], 0, 0, 0);
+        }
+      };
+      block(std::integral_constant<int, 0>{});
+      block(std::integral_constant<int, 1>{});
+      block(std::integral_constant<int, 2>{});
+      block(std::integral_constant<int, 3>{});
+    }
+  }
+  if constexpr (KW > 1) {
+    __syncthreads();
+    f32x4v* join = reinterpret_cast<f32x4v*>(smem) + (size_t)(wave / KW) * RU * NT * 64 + lane;
+    if (kw == 1) {
+#pragma unroll
+      for (int r = 0; r < RU; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) join[(r * NT + t) * 64] = acc[r][t];
+    }
+    __syncthreads();
+    if (kw == 1) return;
+#pragma unroll
+    for (int r = 0; r < RU; ++r)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[r][t] += join[(r * NT + t) * 64];
+  }
+  // acc[r][t]: token 16 t + lane % 16, rows 16 r + 4 (lane / 16) ...
+  float* out = static_cast<float*>(y);
+#pragma unroll
+  for (int r = 0; r < RU; ++r)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int token = 16 * t + (lane & 15), n = row0 + 16 * r + 4 * q;
+      if (token >= T || n >= rows) continue;
+      const size_t at = (size_t)token * rows + n;
+      const f32x4v v = acc[r][t];
+      if (rows % 4 != 0) {
+        for (int e = 0; e < 4 && n + e < rows; ++e) {
+          if (y_bf16)
+            static_cast<__bf16*>(y)[at + e] = (__bf16)v[e];
+          else
+            out[at + e] = v[e];
+        }
+      } else if (y_bf16) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(y) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+      } else {
+        *reinterpret_cast<float4*>(out + at) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    }
 }
 
 // ---- many tokens, packed ----------------------------------------------------------
@@ -194,17 +505,86 @@ __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t* __restrict__ 
   }
 }
 
-template <bool PACKED, int NT, int RU>
+bool whole_words(const MxProduct& p) { return p.cols % 128 == 0 && reinterpret_cast<uintptr_t>(p.scales) % 4 == 0; }
+
+// How the rows are divided: RU sixteens of them for a workgroup, WAVES waves for their columns in turns of TURN steps.  More rows
+// share what is read of the tokens (16 kB per step of 64 tokens, against 1 kB of sixteen rows), but 256 workgroups should be left;
+// where they are fewer, the columns are split too, and the parts joined.
+struct FewShape {
+  int groups, waves, turn;
+};
+FewShape few_shape(int rows) {
+  const int sixteens = (rows + 15) / 16;
+  if (sixteens >= 4 * 256) return {4, 4, 4};
+  return sixteens >= 2 * 256 ? FewShape{2, 8, 1} : FewShape{1, 16, 1};
+}
+int few_splits(int T, int rows, int cols) {
+  const FewShape f = few_shape(rows);
+  const int workgroups = (rows + 16 * f.groups - 1) / (16 * f.groups), turns = (cols + 128 * f.turn - 1) / (128 * f.turn);
+  const int fill = 256 / workgroups, most = turns / f.waves;  // a turn for every wave
+  const int splits = T <= 16 ? 1 : (fill < most ? fill : most);
+  return splits < 1 ? 1 : splits;
+}
+
+template <bool PACKED, int NT, int RU, int WAVES, int TURN>
 hipError_t launch_few(const MxProduct& p, hipStream_t s) {
-  return launch(&k_mx_few<PACKED, NT, RU>, dim3((unsigned)((p.rows + 16 * RU - 1) / (16 * RU))), dim3(64 * kFewWaves), 0, s,
-                p.codes, p.scales, p.x, p.x_scales, p.T, p.rows, p.cols, p.y, p.y_bf16);
+  const int splits = few_splits(p.T, p.rows, p.cols);
+  float* part = static_cast<float*>(p.workspace);
+  const hipError_t e = launch(&k_mx_few<PACKED, NT, RU, WAVES, TURN>,
+                              dim3((unsigned)((p.rows + 16 * RU - 1) / (16 * RU)), (unsigned)splits), dim3(64 * WAVES), 0, s, p.codes,
+                              p.scales, p.x, p.x_scales, p.T, p.rows, p.cols, whole_words(p) ? 1 : 0, p.y, p.y_bf16, part);
+  if (e != hipSuccess || splits == 1) return e;
+  return launch_join_parts(part, p.y, p.y_bf16 != 0, splits, (long long)p.T * p.rows, s);
+}
+
+template <int LPR, int SPAN>
+hipError_t launch_one(const MxProduct& p, hipStream_t s) {
+  const int batch = kWave / LPR * kOneRows, batches = (p.rows + batch - 1) / batch, most = 4096 / SPAN;
+  return launch(&k_mx_one<LPR, SPAN>, dim3((unsigned)(batches < most ? batches : most)), dim3(64 * SPAN), 0, s, p.codes, p.scales,
+                static_cast<const uint16_t*>(p.x), p.rows, p.cols, p.y, p.y_bf16);
+}
+constexpr int kOneMaxCols = 16 * 2048;
+hipError_t launch_one_token(const MxProduct& p, hipStream_t s) {
+  const int blocks = p.cols / kMxBlock;
+  if (blocks <= 8) return launch_one<8, 1>(p, s);
+  if (blocks <= 16) return launch_one<16, 1>(p, s);
+  if (blocks <= 32) return launch_one<32, 1>(p, s);
+  if (blocks <= 64) return launch_one<64, 1>(p, s);
+  if (blocks <= 128) return launch_one<64, 2>(p, s);
+  if (blocks <= 256) return launch_one<64, 4>(p, s);
+  return launch_one<64, 16>(p, s);
+}
+
+template <int NT, int RU, int RW, int KW>
+hipError_t launch_shared(const MxProduct& p, hipStream_t s) {
+  return launch(&k_mx_shared<NT, RU, RW, KW>, dim3((unsigned)((p.rows + 16 * RU * RW - 1) / (16 * RU * RW))), dim3(64 * RW * KW), 0, s,
+                p.codes, p.scales, static_cast<const uint16_t*>(p.x), p.T, p.rows, p.cols, whole_words(p) ? 1 : 0, p.y, p.y_bf16);
+}
+
+// Tokens shared in LDS where the rows still fill the chip in workgroups of 128 or 256.  2048 columns, us through the L2 / shared:
+// 256000 rows, four tokens 69 / 71, sixteen 80 / 72, 33 127 / 86, 64 247 / 103; 32768 rows of 4096, sixteen 23.3 / 22.9, 33 35.2 /
+// 27.4, 64 53.9 / 31.5; 16384 rows, 33 12.5 / 15.5, 64 17.1 / 16.9.
+template <bool PACKED, int NT>
+hipError_t launch_few_by_rows(const MxProduct& p, hipStream_t s) {
+  if constexpr (!PACKED) {
+    if (p.rows >= 256 * 256 && p.T > 4) return launch_shared<NT, 2, 8, 1>(p, s);
+    if constexpr (NT > 1)
+      if (p.rows >= 128 * 256) return launch_shared<NT, 2, 4, 2>(p, s);
+  }
+  const int groups = few_shape(p.rows).groups;
+  if (groups == 4) return launch_few<PACKED, NT, 4, 4, 4>(p, s);
+  return groups == 2 ? launch_few<PACKED, NT, 2, 8, 1>(p, s) : launch_few<PACKED, NT, 1, 16, 1>(p, s);
 }
 template <bool PACKED>
 hipError_t launch_few_tokens(const MxProduct& p, hipStream_t s) {
-  const int nt = (p.T + 15) / 16;
-  if (nt == 1) return p.rows >= 32768 ? launch_few<PACKED, 1, 4>(p, s) : launch_few<PACKED, 1, 2>(p, s);
-  if (nt == 2) return launch_few<PACKED, 2, 2>(p, s);
-  return launch_few<PACKED, 4, 2>(p, s);
+  if constexpr (!PACKED)
+    if (p.T == 1 && p.cols <= kOneMaxCols) return launch_one_token(p, s);
+  switch ((p.T + 15) / 16) {
+    case 1: return launch_few_by_rows<PACKED, 1>(p, s);
+    case 2: return launch_few_by_rows<PACKED, 2>(p, s);
+    case 3: return launch_few_by_rows<PACKED, 3>(p, s);
+    default: return launch_few_by_rows<PACKED, 4>(p, s);
+  }
 }
 
 }  // namespace
@@ -227,9 +607,11 @@ bool mx_pads_scales(const MxProduct& p) {
 }
 }  // namespace
 
-// Room for the padded scale bytes, whether this call's pointers need them or not.
+// Room for the parts of few tokens' sums, or for the padded scale bytes, whether this call's pointers need them or not.
 size_t mx_workspace_bytes(int T, int rows, int cols) {
-  return T <= kMxFewTokens ? 0 : ((size_t)T + rows) * ((cols / kMxBlock + 3) / 4) * 4;
+  if (T > kMxFewTokens) return ((size_t)T + rows) * ((cols / kMxBlock + 3) / 4) * 4;
+  const int splits = few_splits(T, rows, cols);
+  return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0;
 }
 
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
