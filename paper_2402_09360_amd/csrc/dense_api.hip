@@ -152,7 +152,7 @@ int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const voi
 size_t hire_verify_draft_workspace_bytes(const hire_drafts* D) {
   if (check_drafts(D) != HIRE_OK) return 0;
   if (D->target_idx) return kAlign;
-  return align_up((size_t)D->B * draft_parts(D->B, D->vocab).count * 2 * sizeof(double));
+  return align_up(draft_part_bytes(D->B, D->vocab));
 }
 
 int hire_verify_draft(const hire_drafts* D, int32_t* tokens_out, int32_t* accepted_out, void* workspace,

@@ -534,13 +534,14 @@ struct DraftArgs {
   const float* sample_u;      // [B]
   int32_t* out_tokens;        // [B, n + 1]
   int32_t* accepted;          // [B]
-  double* part;               // dense target: sums of the parts, a pair each
+  double* part;               // dense target: draft_part_bytes, sums of the slices of the parts, a pair each
   int parts, part_size;       // set by launch_verify
 };
 struct DraftParts {
   int count, size;
 };
 DraftParts draft_parts(int B, int vocab);  // dense target
+size_t draft_part_bytes(int B, int vocab);
 hipError_t launch_verify(DraftArgs a, hipStream_t s);
 
 // The HIP error behind the calling thread's most recent HIRE_ELAUNCH (api.hip).

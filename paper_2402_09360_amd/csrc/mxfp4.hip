@@ -507,19 +507,23 @@ __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t* __restrict__ 
 
 bool whole_words(const MxProduct& p) { return p.cols % 128 == 0 && reinterpret_cast<uintptr_t>(p.scales) % 4 == 0; }
 
-// How the rows are divided: RU sixteens of them for a workgroup, WAVES waves for their columns in turns of TURN steps.  More rows
-// share what is read of the tokens (16 kB per step of 64 tokens, against 1 kB of sixteen rows), but 256 workgroups should be left;
-// where they are fewer, the columns are split too, and the parts joined.
+// How the rows are divided: `groups` sixteens of them for a workgroup, whose waves take the columns in turns of `turn` steps.  More
+// rows share what is read of the tokens (16 kB per step of 64 tokens, against 1 kB of sixteen rows), but 256 workgroups should
+// be left; beyond sixteen tokens the columns are split where they are fewer, and the parts joined.  us with 4 groups, 8 waves / 2, 8 /
+// 1, 16 (and 4, 4 in turns of four): 64 tokens, 1000 rows of 4096 14.4 / 11.3 / 12.9, 2500 15.4 / 13.3 / 19.0, 5000 18.2 / 22.0 / 36.6, of 1024 11.9 / 8.7 /
+// 12.8, 9000 of 4096 28.0 / 42.5 / 54.2, 16384 29.8 / 43.6 / 73.3 (29.0),
+// of 2048 18.6 / - / - (17.1); 20 tokens, 9000 of 1024 7.0 / 7.4 / 9.3, 2500 6.7 / 6.1 / 6.1.
 struct FewShape {
   int groups, waves, turn;
 };
-FewShape few_shape(int rows) {
+FewShape few_shape(int T, int rows) {
   const int sixteens = (rows + 15) / 16;
-  if (sixteens >= 4 * 256) return {4, 4, 4};
+  if (sixteens >= 4 * 256) return FewShape{4, 4, 4};
+  if (T > 16) return sixteens >= 2 * 256 ? FewShape{4, 8, 1} : FewShape{2, 8, 1};
   return sixteens >= 2 * 256 ? FewShape{2, 8, 1} : FewShape{1, 16, 1};
 }
 int few_splits(int T, int rows, int cols) {
-  const FewShape f = few_shape(rows);
+  const FewShape f = few_shape(T, rows);
   const int workgroups = (rows + 16 * f.groups - 1) / (16 * f.groups), turns = (cols + 128 * f.turn - 1) / (128 * f.turn);
   const int fill = 256 / workgroups, most = turns / f.waves;  // a turn for every wave
   const int splits = T <= 16 ? 1 : (fill < most ? fill : most);
@@ -564,16 +568,17 @@ hipError_t launch_shared(const MxProduct& p, hipStream_t s) {
 // Tokens shared in LDS where the rows still fill the chip in workgroups of 128 or 256.  2048 columns, us through the L2 / shared:
 // 256000 rows, four tokens 69 / 71, sixteen 80 / 72, 33 127 / 86, 64 247 / 103; 32768 rows of 4096, sixteen 23.3 / 22.9, 33 35.2 /
 // 27.4, 64 53.9 / 31.5; 16384 rows, 33 12.5 / 15.5, 64 17.1 / 16.9.
-template <bool PACKED, int NT>
+template <bool PACKED, int NT>  // NT: sixteens of tokens
 hipError_t launch_few_by_rows(const MxProduct& p, hipStream_t s) {
   if constexpr (!PACKED) {
     if (p.rows >= 256 * 256 && p.T > 4) return launch_shared<NT, 2, 8, 1>(p, s);
     if constexpr (NT > 1)
       if (p.rows >= 128 * 256) return launch_shared<NT, 2, 4, 2>(p, s);
   }
-  const int groups = few_shape(p.rows).groups;
-  if (groups == 4) return launch_few<PACKED, NT, 4, 4, 4>(p, s);
-  return groups == 2 ? launch_few<PACKED, NT, 2, 8, 1>(p, s) : launch_few<PACKED, NT, 1, 16, 1>(p, s);
+  const FewShape f = few_shape(p.T, p.rows);
+  if (f.turn == 4) return launch_few<PACKED, NT, 4, 4, 4>(p, s);
+  if constexpr (NT > 1) return f.groups == 4 ? launch_few<PACKED, NT, 4, 8, 1>(p, s) : launch_few<PACKED, NT, 2, 8, 1>(p, s);
+  return f.groups == 2 ? launch_few<PACKED, NT, 2, 8, 1>(p, s) : launch_few<PACKED, NT, 1, 16, 1>(p, s);
 }
 template <bool PACKED>
 hipError_t launch_few_tokens(const MxProduct& p, hipStream_t s) {

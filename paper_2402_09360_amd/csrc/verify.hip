@@ -7,18 +7,27 @@
 #include "kernels.h"
 #include "select.h"
 
+#include <type_traits>
+
 namespace hire {
 namespace {
 
-constexpr int kVerifyThreads = 1024;  // one workgroup for a sequence
-constexpr int kPartThreads = 256;     // workgroups that sum a part of a dense row
+constexpr int kVerifyThreads = 256;  // one workgroup for a sequence; or that sums a part of a dense row
+constexpr int kVerifyWaves = kVerifyThreads / kWave;
+constexpr int kPartSlices = kVerifyWaves;  // of a part, one per wave
 
 // Probability of a token by the first entry of a list that names it; whole wave, every lane gets it.
 __device__ __forceinline__ float list_at(const float* prob, const int32_t* idx, int k, int token) {
-  for (int j0 = 0; j0 < k; j0 += kWave) {
-    const int j = j0 + lane_id();
-    const uint64_t hit = __ballot(j < k && idx[min(j, k - 1)] == token);
-    if (hit != 0ull) return prob[j0 + __builtin_ctzll(hit)];
+  constexpr int kAhead = 8;  // loads under way
+  for (int j0 = 0; j0 < k; j0 += kWave * kAhead) {
+    int32_t name[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) name[u] = idx[min(j0 + u * kWave + lane_id(), k - 1)];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint64_t hit = __ballot(j0 + u * kWave + lane_id() < k && name[u] == token);
+      if (hit != 0ull) return prob[j0 + u * kWave + __builtin_ctzll(hit)];
+    }
   }
   return 0.0f;
 }
@@ -71,44 +80,61 @@ __device__ __forceinline__ int accepted_tokens(const DraftArgs& a, int b, int le
   return mask == 0ull ? length : __builtin_ctzll(mask);
 }
 
-// Sum over the workgroup's threads in front of this one, and of all of them; in a fixed order.  waves: LDS, a value per wave.
-__device__ __forceinline__ double block_prefix(double v, double* waves, double* total) {
-  const double incl = wave_prefix(v, 0.0, [](double x, double y) { return x + y; });
-  if (lane_id() == kWave - 1) waves[wave_id()] = incl;
+// Two sums over the workgroup's threads, in front of each thread and of all of them, in a fixed order.
+struct Running {
+  double before[2], total[2];
+};
+__device__ __forceinline__ Running running_sums(double x, double y, double (&waves)[2][kVerifyWaves]) {
+  auto add = [](double p, double q) { return p + q; };
+  const double ix = wave_prefix(x, 0.0, add), iy = wave_prefix(y, 0.0, add);
+  if (lane_id() == kWave - 1) waves[0][wave_id()] = ix, waves[1][wave_id()] = iy;
   __syncthreads();
-  double before = 0.0, all = 0.0;
-  for (int w = 0; w < (int)(blockDim.x / kWave); ++w) {
-    if (w == wave_id()) before = all;
-    all += waves[w];
+  Running r{{0.0, 0.0}, {0.0, 0.0}};
+#pragma unroll
+  for (int w = 0; w < kVerifyWaves; ++w) {
+    if (w == wave_id()) r.before[0] = r.total[0], r.before[1] = r.total[1];
+    r.total[0] += waves[0][w];
+    r.total[1] += waves[1][w];
   }
-  __syncthreads();
-  *total = all;
-  const double excl = incl - v;  // only a starting point: the picking below takes the first place beyond the mark
-  return before + excl;
+  // a starting point only, which may be off in its last place: the search takes the first value that goes beyond the mark
+  r.before[0] += ix - x;
+  r.before[1] += iy - y;
+  return r;
 }
 
-// The first of this workgroup's places whose running sum is beyond `mark`, else the last place that counts at all.  A thread has
-// the places first + 0 ... count - 1, in order; weight(i) is that of place i.  found: two LDS words.
-template <typename Weight>
-__device__ __forceinline__ int pick_place(double before, double mark, int first, int count, Weight weight, int* found) {
-  if (threadIdx.x == 0) found[0] = 0x7FFFFFFF, found[1] = -1;
-  __syncthreads();
+// Thread t has the values w[0 ... EACH - 1] of places EACH t ...; the first place whose running sum is beyond the mark, else the
+// last one with a positive value, else -1.  *start: the running sum in front of it.
+struct Found {
+  int hit, last;
+  double before_hit, before_last;
+};
+template <int EACH>
+__device__ __forceinline__ int find_place(const double (&w)[EACH], double before, double mark, Found (&waves)[kVerifyWaves],
+                                          double* start) {
+  Found f{-1, -1, 0.0, 0.0};
   double sum = before;
-  int last = -1, hit = 0x7FFFFFFF;
-  for (int i = 0; i < count; ++i) {
-    const double w = weight(first + i);
-    if (!(w > 0.0)) continue;
-    sum += w;
-    last = first + i;
-    if (sum > mark) {
-      hit = last;
-      break;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e)
+    if (w[e] > 0.0) {
+      f.last = (int)threadIdx.x * EACH + e;
+      f.before_last = sum;
+      sum += w[e];
+      if (f.hit < 0 && sum > mark) f.hit = f.last, f.before_hit = f.before_last;
     }
-  }
-  if (hit != 0x7FFFFFFF) atomicMin(&found[0], hit);
-  if (last >= 0) atomicMax(&found[1], last);
+  const uint64_t hits = __ballot(f.hit >= 0), any = __ballot(f.last >= 0);
+  const int h = hits ? (int)__builtin_ctzll(hits) : 0, l = any ? 63 - (int)__builtin_clzll(any) : 0;
+  f = Found{read_lane(f.hit, h), read_lane(f.last, l), read_lane(f.before_hit, h), read_lane(f.before_last, l)};
+  if (lane_id() == 0) waves[wave_id()] = f;
   __syncthreads();
-  return found[0] != 0x7FFFFFFF ? found[0] : found[1];
+  Found r{-1, -1, 0.0, 0.0};
+#pragma unroll
+  for (int v = kVerifyWaves - 1; v >= 0; --v) {
+    const Found o = waves[v];
+    if (o.hit >= 0) r.hit = o.hit, r.before_hit = o.before_hit;
+    if (r.last < 0 && o.last >= 0) r.last = o.last, r.before_last = o.before_last;
+  }
+  *start = r.hit >= 0 ? r.before_hit : r.before_last;
+  return r.hit >= 0 ? r.hit : r.last;
 }
 
 __device__ __forceinline__ void write_tokens(const DraftArgs& a, int b, int accepted, int next) {
@@ -145,49 +171,54 @@ struct PlaceTable {
   }
 };
 
-constexpr int kListEach = kMaxDraftList / kVerifyThreads;
-
+template <int EACH>  // places of a thread
 __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
-  __shared__ int ok[kMaxDraft], found[2];
-  __shared__ double waves[kVerifyThreads / kWave];
-  __shared__ int32_t keys[2 * kMaxDraftList], places[2 * kMaxDraftList];
+  constexpr int kSlots = 2 * EACH * kVerifyThreads;
+  __shared__ int ok[kMaxDraft];
+  __shared__ double waves[2][kVerifyWaves];
+  __shared__ Found found[kVerifyWaves];
+  __shared__ int32_t keys[kSlots], places[kSlots];
   const int b = blockIdx.x, length = draft_length(a, b);
+  const double sample = (double)a.sample_u[b];
+  const PlaceTable table{keys, places, kSlots - 1};
+  table.clear();
   const int accepted = accepted_tokens(a, b, length, ok);
   const float* p = target_row(a, b, accepted);
   const int32_t* tokens = target_list(a, b, accepted);
-  const bool refused = accepted < length;
-  const int each = (a.target_k + kVerifyThreads - 1) / kVerifyThreads, first = (int)threadIdx.x * each;
-  const int count = min(max(a.target_k - first, 0), each);
+  const bool refused = accepted < length, by_list = refused && a.draft_idx;
+  const int first = (int)threadIdx.x * EACH;
 
-  PlaceTable table{keys, places, 63};
-  const int longest = max(a.target_k, a.draft_idx ? a.draft_k : 0);
-  while (table.mask + 1 < 2 * longest) table.mask = 2 * table.mask + 1;
-  table.clear();
-  int token[kListEach];
-  double whole[kListEach], rest[kListEach];
+  int token[EACH], other[EACH];
+  double whole[EACH], rest[EACH];
 #pragma unroll
-  for (int i = 0; i < kListEach; ++i) {
-    const bool there = i < count;
-    token[i] = there ? tokens[first + i] : -1;
-    whole[i] = there ? (double)p[first + i] : 0.0;
-    if ((unsigned)token[i] >= (unsigned)a.vocab) token[i] = -1;
+  for (int i = 0; i < EACH; ++i) {
+    const int at = min(first + i, a.target_k - 1);
+    token[i] = tokens[at];
+    whole[i] = (double)p[at];
+    if (by_list) other[i] = draft_list(a, b, accepted)[min((int)threadIdx.x + i * kVerifyThreads, a.draft_k - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    if (first + i >= a.target_k || (unsigned)token[i] >= (unsigned)a.vocab) token[i] = -1;
     if (token[i] >= 0) table.insert(token[i], first + i);
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kListEach; ++i)
+  for (int i = 0; i < EACH; ++i)
     if (token[i] < 0 || table.find(token[i]) != first + i || !(whole[i] > 0.0)) whole[i] = 0.0, token[i] = -1;
-  __syncthreads();
-  if (refused && a.draft_idx) {
+  if (by_list) {
+    __syncthreads();
     table.clear();
-    const int32_t* list = draft_list(a, b, accepted);
-    for (int j = threadIdx.x; j < a.draft_k; j += kVerifyThreads)
-      if ((unsigned)list[j] < (unsigned)a.vocab) table.insert(list[j], j);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int j = (int)threadIdx.x + i * kVerifyThreads;
+      if (j < a.draft_k && (unsigned)other[i] < (unsigned)a.vocab) table.insert(other[i], j);
+    }
     __syncthreads();
   }
   double sums[2] = {0.0, 0.0};
 #pragma unroll
-  for (int i = 0; i < kListEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     double q = 0.0;
     if (refused && token[i] >= 0) {
       if (a.draft_idx) {
@@ -203,21 +234,138 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
     sums[0] += rest[i];
     sums[1] += whole[i];
   }
-  double total, total_whole;
-  double before = block_prefix(sums[0], waves, &total);
-  const double before_whole = block_prefix(sums[1], waves, &total_whole);
-  const bool nothing = !(total > 0.0);  // the draft's covers the target's everywhere: the target's itself
-  if (nothing) before = before_whole, total = total_whole;
-  const double mark = (double)a.sample_u[b] * total;
-  auto weight = [&](int at) {
-    double w = 0.0;
+  const Running r = running_sums(sums[0], sums[1], waves);
+  const bool nothing = !(r.total[0] > 0.0);  // the draft's covers the target's everywhere: the target's itself
 #pragma unroll
-    for (int i = 0; i < kListEach; ++i)
-      if (at == first + i) w = nothing ? whole[i] : rest[i];
-    return w;
-  };
-  const int at = pick_place(before, mark, first, count, weight, found);
+  for (int i = 0; i < EACH; ++i) rest[i] = nothing ? whole[i] : rest[i];
+  double start;
+  const int at = find_place<EACH>(rest, nothing ? r.before[1] : r.before[0], sample * (nothing ? r.total[1] : r.total[0]), found,
+                                  &start);
   write_tokens(a, b, accepted, at >= 0 ? tokens[at] : -1);
+}
+
+// Short lists (or a draft that was certain): a wave for every position takes its lists into registers before it is known which
+// positions are reached, so that everything is asked for at once; the wave of the position behind the accepted tokens then does
+// the rest alone.  Eight sequences of four drafted tokens with lists of 64: LISTS_US.
+constexpr int kShortEach = 4;                       // entries of a lane
+constexpr int kShortList = kShortEach * kWave;      // longest list
+constexpr int kShortWaves = 16;                     // most positions
+template <int EACH>
+struct ShortList {
+  int token[EACH];
+  float prob[EACH];
+  __device__ __forceinline__ void load(const float* p, const int32_t* idx, int k, bool there) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int j = e * kWave + lane_id(), at = there && j < k ? j : 0;
+      token[e] = idx[at];
+      prob[e] = p[at];
+      if (!there || j >= k) token[e] = -1, prob[e] = 0.0f;
+    }
+  }
+  // Probability of `wanted` by the first entry that names it.
+  __device__ __forceinline__ float find(int wanted) const {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const uint64_t hit = __ballot(token[e] == wanted);
+      if (hit != 0ull) return read_lane(prob[e], (int)__builtin_ctzll(hit));
+    }
+    return 0.0f;
+  }
+};
+
+template <int EACH>
+__global__ __launch_bounds__(kWave* kShortWaves) void k_verify_short(DraftArgs a) {
+  __shared__ int ok[kShortWaves];
+  __shared__ int32_t keys[2 * kShortList], places[2 * kShortList];
+  const int b = blockIdx.x, i = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id();
+  const bool drafted = i < a.n;
+  const size_t at = (size_t)b * a.n + (drafted ? i : 0);
+  ShortList<EACH> p, q;
+  p.load(target_row(a, b, i), target_list(a, b, i), a.target_k, true);
+  if (a.draft) q.load(draft_row(a, b, drafted ? i : 0), draft_list(a, b, drafted ? i : 0), a.draft_k, drafted);
+  const int length = draft_length(a, b), token = drafted ? a.tokens[at] : -1;
+  const float u = drafted ? a.accept_u[at] : 0.0f, mark_at = a.sample_u[b];
+  int yes = 0;
+  if (i < length && (unsigned)token < (unsigned)a.vocab)
+    yes = (double)u * (a.draft ? (double)q.find(token) : 1.0) < (double)p.find(token) ? 1 : 0;
+  if (lane == 0) ok[i] = yes;
+  __syncthreads();
+  const uint64_t refusals = __ballot(lane < length && ok[min(lane, kShortWaves - 1)] == 0);
+  const int accepted = refusals == 0ull ? length : (int)__builtin_ctzll(refusals);
+  int32_t* out = a.out_tokens + (size_t)b * (a.n + 1);
+  if (i != accepted) {
+    if (lane == 0) out[i] = i < accepted ? token : -1;
+    return;
+  }
+  // this wave alone from here on: LDS in the order of the program
+  const bool refused = accepted < length;
+  PlaceTable table{keys, places, 2 * kWave * EACH - 1};
+  auto clear = [&]() {
+    for (int j = lane; j <= table.mask; j += kWave) keys[j] = -1, places[j] = 0x7FFFFFFF;
+    __builtin_amdgcn_wave_barrier();
+  };
+  clear();
+  double whole[EACH], rest[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e)
+    if ((unsigned)p.token[e] < (unsigned)a.vocab) table.insert(p.token[e], e * kWave + lane);
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const bool first = (unsigned)p.token[e] < (unsigned)a.vocab && table.find(p.token[e]) == e * kWave + lane;
+    whole[e] = first && p.prob[e] > 0.0f ? (double)p.prob[e] : 0.0;
+    rest[e] = whole[e];
+  }
+  if (refused && !a.draft) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if (p.token[e] == token) rest[e] = fmax(whole[e] - 1.0, 0.0);
+  } else if (refused) {
+    __builtin_amdgcn_wave_barrier();
+    clear();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if ((unsigned)q.token[e] < (unsigned)a.vocab) table.insert(q.token[e], e * kWave + lane);
+    __builtin_amdgcn_wave_barrier();
+    float* probs = reinterpret_cast<float*>(keys);  // by place, once the places are found
+    int found[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) found[e] = whole[e] > 0.0 ? table.find(p.token[e]) : 0x7FFFFFFF;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) probs[e * kWave + lane] = q.prob[e];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if (found[e] != 0x7FFFFFFF) rest[e] = fmax(whole[e] - (double)probs[found[e]], 0.0);
+  }
+  // running sums in the order of the places: blocks of 64 one after the other
+  auto pick = [&](const double (&w)[EACH], int* next) {
+    double sums[EACH], total = 0.0;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      sums[e] = total + wave_prefix(w[e], 0.0, [](double x, double y) { return x + y; });
+      total = read_lane63(sums[e]);
+    }
+    if (!(total > 0.0)) return false;
+    const double mark = (double)mark_at * total;
+    int last = -1;
+#pragma unroll
+    for (int e = EACH - 1; e >= 0; --e) {
+      const uint64_t beyond = __ballot(w[e] > 0.0 && sums[e] > mark), any = __ballot(w[e] > 0.0);
+      if (beyond != 0ull) *next = read_lane(p.token[e], (int)__builtin_ctzll(beyond)), last = -2;
+      if (last == -1 && any != 0ull) last = e;
+      if (last == e) *next = read_lane(p.token[e], 63 - (int)__builtin_clzll(any));
+    }
+    return true;
+  };
+  int next = -1;
+  if (!pick(rest, &next)) pick(whole, &next);
+  if (lane == 0) {
+    out[i] = next;
+    a.accepted[b] = accepted;
+  }
 }
 
 // ---- target dense: parts of the row in workgroups of their own, then one per sequence --------
@@ -263,95 +411,163 @@ __device__ __forceinline__ PartDraft<KIND> part_draft(const DraftArgs& a, int b,
   return d;
 }
 
-template <int KIND>
-__global__ __launch_bounds__(kPartThreads) void k_verify_sums(DraftArgs a) {
+// A wave sums a quarter of the workgroup's part, so that the one behind has less to look through; the first workgroup of a
+// sequence leaves how many tokens were accepted.  VEC: rows start at multiples of 16 bytes.
+template <int KIND, bool VEC>
+__global__ __launch_bounds__(kVerifyThreads) void k_verify_sums(DraftArgs a) {
   __shared__ int ok[kMaxDraft];
-  __shared__ double waves[2][kPartThreads / kWave];
   __shared__ int32_t places[KIND == kDraftList ? kMaxDraftPart : 1];
   const int b = blockIdx.y, length = draft_length(a, b);
   const int accepted = accepted_tokens(a, b, length, ok);
-  const int v0 = blockIdx.x * a.part_size, v1 = min(v0 + a.part_size, a.vocab);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.accepted[b] = accepted;
+  const int v0 = blockIdx.x * a.part_size;
   const float* p = target_row(a, b, accepted);
   const PartDraft<KIND> q = part_draft<KIND>(a, b, accepted, accepted < length, v0, a.part_size, places);
+  const int slice = a.part_size / kPartSlices, w0 = v0 + wave_id() * slice, w1 = min(w0 + slice, a.vocab), lane = lane_id();
   double rest = 0.0, whole = 0.0;
-#pragma unroll 8
-  for (int v = v0 + (int)threadIdx.x; v < v1; v += kPartThreads) {
-    const double w = fmax((double)p[v], 0.0);
+  auto add = [&](float pv, double qv) {
+    const double w = fmax((double)pv, 0.0);
     whole += w;
-    rest += fmax(w - q.at(v), 0.0);
+    rest += fmax(w - qv, 0.0);
+  };
+  if constexpr (VEC) {
+    constexpr int kAhead = 4;
+    for (int v = w0 + 4 * lane; v < w1; v += 256 * kAhead) {  // w1 is a multiple of 4
+      float4 pv[kAhead], qv[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int at = min(v + 256 * u, w1 - 4);
+        pv[u] = *reinterpret_cast<const float4*>(p + at);
+        if constexpr (KIND == kDraftDense) qv[u] = *reinterpret_cast<const float4*>((q.refused ? q.row : p) + at);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int at = v + 256 * u;
+        if (at >= w1) break;
+        const float pe[4] = {pv[u].x, pv[u].y, pv[u].z, pv[u].w};
+        if constexpr (KIND == kDraftDense) {
+          const float qe[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) add(pe[e], q.refused ? (double)qe[e] : 0.0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) add(pe[e], q.at(at + e));
+        }
+      }
+    }
+  } else {
+#pragma unroll 8
+    for (int v = w0 + lane; v < w1; v += kWave) add(p[v], q.at(v));
   }
   rest = wave_sum(rest);
   whole = wave_sum(whole);
-  if (lane_id() == 0) waves[0][wave_id()] = rest, waves[1][wave_id()] = whole;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kPartThreads / kWave; ++w) rest += waves[0][w], whole += waves[1][w];
-    double* out = a.part + 2 * ((size_t)b * a.parts + blockIdx.x);
+  if (lane == 0) {
+    double* out = a.part + 2 * (((size_t)b * a.parts + blockIdx.x) * kPartSlices + wave_id());
     out[0] = rest;
     out[1] = whole;
   }
 }
 
+// A workgroup per sequence: the slice of the row in which the running sum passes the mark, then the place in it, whose values stay in
+// registers between the sum and the search.
+constexpr int kMostSlices = 4 * kVerifyThreads;
+
 template <int KIND>
 __global__ __launch_bounds__(kVerifyThreads) void k_verify_pick(DraftArgs a) {
-  __shared__ int ok[kMaxDraft], found[2];
-  __shared__ double waves[kVerifyThreads / kWave], start;
-  __shared__ int32_t places[KIND == kDraftList ? kMaxDraftPart : 1];
-  const int b = blockIdx.x, length = draft_length(a, b);
-  const int accepted = accepted_tokens(a, b, length, ok);
-  const bool mine = (int)threadIdx.x < a.parts;
-  const double* part = a.part + 2 * ((size_t)b * a.parts + (mine ? threadIdx.x : 0));
-  double rest = mine ? part[0] : 0.0;
-  const double whole = mine ? part[1] : 0.0;
-  double total, total_whole;
-  double before = block_prefix(rest, waves, &total);
-  const double before_whole = block_prefix(whole, waves, &total_whole);
-  const bool nothing = !(total > 0.0);
-  if (nothing) before = before_whole, total = total_whole, rest = whole;
-  const double mark = (double)a.sample_u[b] * total;
-  // the part, then the place in it
-  const int at_part = pick_place(before, mark, (int)threadIdx.x, mine ? 1 : 0, [&](int) { return rest; }, found);
-  if ((int)threadIdx.x == at_part) start = before;
-  __syncthreads();
+  constexpr int kSlices = kMostSlices / kVerifyThreads, kEach = kMaxDraftPart / kPartSlices / kVerifyThreads;
+  __shared__ double waves[2][2][kVerifyWaves];
+  __shared__ Found found[2][kVerifyWaves];
+  __shared__ int32_t places[KIND == kDraftList ? kMaxDraftPart / kPartSlices : 1];
+  const int b = blockIdx.x, slices = a.parts * kPartSlices, slice = a.part_size / kPartSlices;
+  const double2* part = reinterpret_cast<const double2*>(a.part) + (size_t)b * slices;
+  double w[kSlices], whole[kSlices], sums[2] = {0.0, 0.0};
+#pragma unroll
+  for (int e = 0; e < kSlices; ++e) {
+    const int at = (int)threadIdx.x * kSlices + e;
+    const double2 v = part[min(at, slices - 1)];
+    w[e] = at < slices ? v.x : 0.0;
+    whole[e] = at < slices ? v.y : 0.0;
+  }
+  const int length = draft_length(a, b), accepted = a.accepted[b];
+  const double sample = (double)a.sample_u[b];
+#pragma unroll
+  for (int e = 0; e < kSlices; ++e) sums[0] += w[e], sums[1] += whole[e];
+  const Running r = running_sums(sums[0], sums[1], waves[0]);
+  const bool nothing = !(r.total[0] > 0.0);
+#pragma unroll
+  for (int e = 0; e < kSlices; ++e) w[e] = nothing ? whole[e] : w[e];
+  const double mark = sample * (nothing ? r.total[1] : r.total[0]);
+  double start, unused;
+  const int at_slice = find_place<kSlices>(w, nothing ? r.before[1] : r.before[0], mark, found[0], &start);
   int next = -1;
-  if (at_part >= 0) {
-    const int v0 = at_part * a.part_size, size = min(a.part_size, a.vocab - v0);
-    const float* p = target_row(a, b, accepted);
-    const PartDraft<KIND> q = part_draft<KIND>(a, b, accepted, accepted < length && !nothing, v0, a.part_size, places);
-    const int each = (size + kVerifyThreads - 1) / kVerifyThreads, first = v0 + (int)threadIdx.x * each;
-    const int count = min(max(v0 + size - first, 0), each);
-    auto weight = [&](int v) { return fmax(fmax((double)p[v], 0.0) - q.at(v), 0.0); };
-    double sum = 0.0, all;
-    for (int i = 0; i < count; ++i) sum += weight(first + i);
-    const double inside = block_prefix(sum, waves, &all);
-    next = pick_place(start + inside, mark, first, count, weight, found);
+  if (at_slice >= 0) {
+    const int v0 = at_slice * slice, size = min(slice, a.vocab - v0), first = (int)threadIdx.x * kEach;
+    const float* p = target_row(a, b, accepted) + v0;
+    const PartDraft<KIND> q = part_draft<KIND>(a, b, accepted, accepted < length && !nothing, v0, slice, places);
+    double x[kEach], sum = 0.0;
+    // neighbouring threads load neighbouring values; in the order of the places they go through LDS
+    __shared__ float staged[kMaxDraftPart / kPartSlices];
+    float pv[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) pv[i] = p[min((int)threadIdx.x + i * kVerifyThreads, size - 1)];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = (int)threadIdx.x + i * kVerifyThreads;
+      if (at < slice) staged[at] = at < size ? (float)pv[i] : 0.0f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      x[i] = first + i < size ? fmax(fmax((double)staged[first + i], 0.0) - q.at(v0 + first + i), 0.0) : 0.0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += x[i];
+    const Running in = running_sums(sum, 0.0, waves[1]);
+    next = find_place<kEach>(x, start + in.before[0], mark, found[1], &unused);
+    if (next >= 0) next += v0;
   }
   write_tokens(a, b, accepted, next);
 }
 
 }  // namespace
 
-// Parts of a dense row: about a thousand workgroups over the batch, none with fewer than 1024 tokens.
+// Parts of a dense row: about a thousand workgroups over the batch, of at least 1024 tokens; the slices of all of them are
+// what the workgroup that picks holds.
 DraftParts draft_parts(int B, int vocab) {
   int parts = 1024 / B;
-  parts = parts < 16 ? 16 : (parts > 256 ? 256 : parts);
+  parts = parts < 16 ? 16 : (parts > kMostSlices / kPartSlices ? kMostSlices / kPartSlices : parts);
   int size = ((vocab + parts - 1) / parts + 1023) / 1024 * 1024;
   if (size > kMaxDraftPart) size = kMaxDraftPart;
   return DraftParts{(vocab + size - 1) / size, size};
 }
+size_t draft_part_bytes(int B, int vocab) { return (size_t)B * draft_parts(B, vocab).count * kPartSlices * 2 * sizeof(double); }
 
 hipError_t launch_verify(DraftArgs a, hipStream_t s) {
-  if (a.target_idx) return launch(&k_verify_lists, dim3((unsigned)a.B), dim3(kVerifyThreads), 0, s, a);
+  if (a.target_idx) {
+    const int longest = a.draft_idx && a.draft_k > a.target_k ? a.draft_k : a.target_k;
+    if (longest <= kShortList && a.n < kShortWaves && (!a.draft || a.draft_idx)) {
+      const dim3 grid((unsigned)a.B), block((unsigned)(kWave * (a.n + 1)));
+      return longest <= kWave ? launch(&k_verify_short<1>, grid, block, 0, s, a) : launch(&k_verify_short<kShortEach>, grid, block, 0, s, a);
+    }
+    const dim3 grid((unsigned)a.B), block(kVerifyThreads);
+    if (longest <= 2 * kVerifyThreads) return launch(&k_verify_lists<2>, grid, block, 0, s, a);
+    return launch(longest <= 4 * kVerifyThreads ? &k_verify_lists<4> : &k_verify_lists<kMaxDraftList / kVerifyThreads>, grid, block, 0,
+                  s, a);
+  }
   const DraftParts parts = draft_parts(a.B, a.vocab);
   a.parts = parts.count;
   a.part_size = parts.size;
-  auto both = [&](void (*sums)(DraftArgs), void (*pick)(DraftArgs)) {
-    const hipError_t e = launch(sums, dim3((unsigned)a.parts, (unsigned)a.B), dim3(kPartThreads), 0, s, a);
-    return e != hipSuccess ? e : launch(pick, dim3((unsigned)a.B), dim3(kVerifyThreads), 0, s, a);
+  const bool vec = a.vocab % 4 == 0 && reinterpret_cast<uintptr_t>(a.target) % 16 == 0 &&
+                   (!a.draft || a.draft_idx || reinterpret_cast<uintptr_t>(a.draft) % 16 == 0);
+  auto both = [&](auto kind) {
+    constexpr int KIND = decltype(kind)::value;
+    const dim3 grid((unsigned)a.parts, (unsigned)a.B);
+    const hipError_t e = vec ? launch(&k_verify_sums<KIND, true>, grid, dim3(kVerifyThreads), 0, s, a)
+                             : launch(&k_verify_sums<KIND, false>, grid, dim3(kVerifyThreads), 0, s, a);
+    return e != hipSuccess ? e : launch(&k_verify_pick<KIND>, dim3((unsigned)a.B), dim3(kVerifyThreads), 0, s, a);
   };
-  if (!a.draft) return both(&k_verify_sums<kDraftCertain>, &k_verify_pick<kDraftCertain>);
-  if (!a.draft_idx) return both(&k_verify_sums<kDraftDense>, &k_verify_pick<kDraftDense>);
-  return both(&k_verify_sums<kDraftList>, &k_verify_pick<kDraftList>);
+  if (!a.draft) return both(std::integral_constant<int, kDraftCertain>{});
+  if (!a.draft_idx) return both(std::integral_constant<int, kDraftDense>{});
+  return both(std::integral_constant<int, kDraftList>{});
 }
 
 }  // namespace hire
