@@ -101,21 +101,34 @@ inline hipError_t launch_join_parts(const float* part, void* out, bool bf16, int
                 s, part, out, parts, values);
 }
 
-template <bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
-hipError_t launch_product(const GemmArgs& g, const Epilogue& epi, hipStream_t s) {
-  const int n_tile = PAIR ? kGemmTile / 2 : kGemmTile;
-  const long long tiles = (long long)((g.M + kGemmTile - 1) / kGemmTile) * ((g.N + n_tile - 1) / n_tile);
-  return launch(&k_dense_product<AK, BK, PAIR, MX, Epilogue>, dim3((unsigned)(tiles * g.products * g.splits)), dim3(512), 0, s, g,
-                epi);
+// How a product is cut up: the tile and the parts of k.  In units of a 256 x 256 x 32 stage (about 0.45 us): a tile of 256 takes
+// a compute unit, of 128 half of one, which then yields 0.7 of the rate; a round of tiles has about eight stages' worth of
+// start and epilogue; parts are written and read again, from caches for the most part (8 TB/s), and their join is a kernel (5 us).
+struct ProductShape {
+  int tile, splits;
+};
+inline ProductShape product_shape(int M, int N, int steps, int products, int most_splits) {
+  ProductShape best{256, 1};
+  double least = 0.0;
+  for (int tile = 256; tile >= 128; tile /= 2)
+    for (int splits = 1; splits <= most_splits; ++splits) {
+      if (splits > 1 && steps / splits < 16) break;
+      const double tiles = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * products * splits;
+      const double slots = tile == 256 ? 256.0 : 512.0, rounds = (double)(long long)((tiles + slots - 1.0) / slots);
+      const double stage = tile == 256 ? 1.0 : (tiles <= 256.0 ? 0.4 : 0.72);
+      double cost = rounds * (((steps + splits - 1) / splits) * stage + 8.0);
+      if (splits > 1) cost += 11.0 + 8.0 * splits * M * N / 8e6 / 0.45;
+      if (least == 0.0 || cost < least) least = cost, best = ProductShape{tile, splits};
+    }
+  return best;
 }
 
-// Parts of k for a product of one M x N matrix: as many as fill the chip, each at least sixteen stages long.
-inline int product_splits(int M, int N, int steps) {
-  const long long tiles = (long long)((M + kGemmTile - 1) / kGemmTile) * ((N + kGemmTile - 1) / kGemmTile);
-  int s = (int)(256 / tiles);
-  s = s < 1 ? 1 : s;
-  const int most = steps / 16 < 1 ? 1 : steps / 16;
-  return s < most ? s : most;
+template <bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
+hipError_t launch_product(const GemmArgs& g, int tile, const Epilogue& epi, hipStream_t s) {
+  const int n_tile = PAIR ? tile / 2 : tile;
+  const long long tiles = (long long)((g.M + tile - 1) / tile) * ((g.N + n_tile - 1) / n_tile);
+  return launch(tile == 256 ? &k_dense_product<256, AK, BK, PAIR, MX, Epilogue> : &k_dense_product<128, AK, BK, PAIR, MX, Epilogue>,
+                dim3((unsigned)(tiles * g.products * g.splits)), dim3((unsigned)(2 * tile)), 0, s, g, epi);
 }
 
 }  // namespace hire

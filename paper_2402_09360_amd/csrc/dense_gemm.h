@@ -172,29 +172,34 @@ __device__ __forceinline__ void gemm_barrier() {
 //   Measured against a double buffer of 64 k whose waves run freely (4096 x 4096 x 8192, normal values): 1019 -> 1222
 // TFLOP/s; 79 % of the cycles are the matrix cores' (56 %), and with these values the clock drops to about 1.6 GHz: with
 // zeros the same kernel does 1665.
+//   With one group the only barrier of a stage is the one behind its reads: a wave that requests s + 3 has passed that of s - 1,
+// in front of which every wave's reads of s - 1 were done.
 // An epilogue gets a wave's sums: acc[i][j], rows m of block i at lane % 32, columns n of block j: register r is column
 // 8 (r / 4) + 4 (lane / 32) + r % 4.
 // MX: microscaled operands.  A stage's 64 bytes of a row are 128 columns, four blocks; the row's four scale bytes travel beside
 // them, one word per row of both tiles.  A lane's sixteen bytes of a fragment are one block, whose scale byte the matrix
 // instruction picks from the row's word, shifted by a byte in the upper half of the wave.
-constexpr int kGemmTile = 256;
-template <bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_product(GemmArgs g, Epilogue epi) {
-  constexpr int kWaves = 8, kMB = 4, kNB = 2;
-  using TA = GemmTile<kGemmTile, kWaves, AK, false>;
-  using TB = GemmTile<kGemmTile, kWaves, BK, PAIR>;
+// TILE 128, where there are too few tiles of 256 for the chip: four waves of 64 x 64 in one group; two workgroups of a compute unit
+// fill each other's waits.
+template <int TILE, bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
+__global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_dense_product(GemmArgs g, Epilogue epi) {
+  constexpr int kWaves = TILE / 32, kNW = TILE / 64, kMB = TILE / 64, kNB = 2;
+  constexpr bool kGroups = TILE == 256;
+  static_assert(TILE == 256 || TILE == 128, "two waves of m, the rest of n");
+  using TA = GemmTile<TILE, kWaves, AK, false>;
+  using TB = GemmTile<TILE, kWaves, BK, PAIR>;
   static_assert(!MX || (AK && BK && !PAIR), "rows of codes");
-  constexpr int kCodes = TA::kBytes + TB::kBytes, kStage = kCodes + (MX ? 2 * kGemmTile * 4 : 0);
+  constexpr int kCodes = TA::kBytes + TB::kBytes, kStage = kCodes + (MX ? 2 * TILE * 4 : 0);
   constexpr int kYounger = (kGemmStages - 2) * (TA::kLoads + TB::kLoads + (MX ? 1 : 0));
   __shared__ __align__(1024) char smem[kGemmStages * kStage];
 
-  const int n_tile = PAIR ? kGemmTile / 2 : kGemmTile;
-  const int tiles_m = (g.M + kGemmTile - 1) / kGemmTile, tiles_n = (g.N + n_tile - 1) / n_tile, tiles = tiles_m * tiles_n;
+  const int n_tile = PAIR ? TILE / 2 : TILE;
+  const int tiles_m = (g.M + TILE - 1) / TILE, tiles_n = (g.N + n_tile - 1) / n_tile, tiles = tiles_m * tiles_n;
   const int w = gemm_place((int)blockIdx.x, (int)gridDim.x), z = w / tiles, t = w % tiles;
   const int product = z / g.splits, split = z % g.splits;
   // groups of eight tiles of m, so that the 32 workgroups of a die form a patch
   const int group = t / (8 * tiles_n), in = t % (8 * tiles_n), gm = min(8, tiles_m - 8 * group);
-  const int m0 = (8 * group + in % gm) * kGemmTile, n0 = in / gm * n_tile;
+  const int m0 = (8 * group + in % gm) * TILE, n0 = in / gm * n_tile;
 
   const int seg_steps = (g.K + kGemmStep - 1) / kGemmStep, steps = seg_steps * g.segments;
   const int s0 = (int)((long long)steps * split / g.splits);
@@ -206,12 +211,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   tb.init(n0, g.N, g.ldb);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
   const int wave = __builtin_amdgcn_readfirstlane(wave_id());
-  const char* scales = nullptr;  // MX: waves 0 to 3 those of the first tile's rows, 4 to 7 of the second's
+  const char* scales = nullptr;  // MX: the first half of the waves those of the first tile's rows, the others of the second's
   uint32_t scale_off = 0;
   if constexpr (MX) {
-    const int row0 = wave < 4 ? m0 : n0, last = (wave < 4 ? g.M : g.N) - 1 - row0;
-    scales = reinterpret_cast<const char*>(wave < 4 ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld + 4 * (size_t)s0;
-    scale_off = (uint32_t)min(wave % 4 * 64 + lane_id(), last) * g.scale_ld;
+    const bool of_a = wave < kWaves / 2;
+    const int row0 = of_a ? m0 : n0, last = (of_a ? g.M : g.N) - 1 - row0;
+    scales = reinterpret_cast<const char*>(of_a ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld + 4 * (size_t)s0;
+    scale_off = (uint32_t)min(wave % (kWaves / 2) * 64 + lane_id(), last) * g.scale_ld;
   }
   // the next stage to request: its place, addresses and what is left of its segment of k
   int requested = 0, place = 0, left = 0;
@@ -241,7 +247,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (++requested < n && left <= 0) locate(s0 + requested);
   };
 
-  const int wm = wave / 4 * 128, wn = wave % 4 * 64;
+  const int wm = wave / kNW * (TILE / 2), wn = wave % kNW * 64;
   f32x16v acc[kMB][kNB] = {};
   if (n > 0) locate(s0);
   for (int i = 0; i < kGemmStages - 1 && i < n; ++i) request();
@@ -249,7 +255,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(kYounger) : "memory");
   else
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  if (wave >= 4) gemm_barrier();  // the second group: half a stage later
+  if (kGroups && wave >= 4) gemm_barrier();  // the second group: half a stage later
   int cur = 0;
   for (int s = 0; s < n; ++s) {
     const char* sa = smem + cur * kStage;
@@ -270,7 +276,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int i = 0; i < kMB; ++i) xa[i] = words[wm + 32 * i] >> shift;
 #pragma unroll
-      for (int j = 0; j < kNB; ++j) xb[j] = words[kGemmTile + wn + 32 * j] >> shift;
+      for (int j = 0; j < kNB; ++j) xb[j] = words[TILE + wn + 32 * j] >> shift;
     }
     __builtin_amdgcn_sched_barrier(0);
     if (requested < n) {
@@ -280,7 +286,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     }
     gemm_barrier();
-    __builtin_amdgcn_s_setprio(1);
+    if constexpr (kGroups) __builtin_amdgcn_s_setprio(1);
     auto multiply = [&](auto half) {
       constexpr int KS = decltype(half)::value;
 #pragma unroll
@@ -296,10 +302,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     };
     multiply(std::integral_constant<int, 0>{});
     multiply(std::integral_constant<int, 1>{});
-    __builtin_amdgcn_s_setprio(0);
-    gemm_barrier();
+    if constexpr (kGroups) {
+      __builtin_amdgcn_s_setprio(0);
+      gemm_barrier();
+    }
   }
-  if (wave < 4) gemm_barrier();
+  if (kGroups && wave < 4) gemm_barrier();
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // LDS is the epilogue's
   epi.store(acc, smem, m0 + wm, n0 + (PAIR ? wn / 2 : wn), g.M, g.N, product, split);
 }

@@ -68,13 +68,20 @@ struct StoreGateSlopes {
   }
 };
 
+constexpr int kMostSplits = 32;
+int k_steps(int k) { return (k + kGemmStep - 1) / kGemmStep; }
+ProductShape split_shape(int M, int N, int K, int segments) {
+  return product_shape(M, N, segments * k_steps(K), 1, kMostSplits);
+}
+
 // One product with an M x N bf16 result, split over k where the tiles are few.
 template <bool AK, bool BK>
 hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStream_t s) {
   g.products = 1;
-  g.splits = product_splits(g.M, g.N, g.segments * ((g.K + kGemmStep - 1) / kGemmStep));
-  if (g.splits == 1) return launch_product<AK, BK, false, false>(g, StoreBf16{{out, nullptr, nullptr}}, s);
-  const hipError_t e = launch_product<AK, BK, false, false>(g, StorePart{part}, s);
+  const ProductShape shape = split_shape(g.M, g.N, g.K, g.segments);
+  g.splits = shape.splits;
+  if (g.splits == 1) return launch_product<AK, BK, false, false>(g, shape.tile, StoreBf16{{out, nullptr, nullptr}}, s);
+  const hipError_t e = launch_product<AK, BK, false, false>(g, shape.tile, StorePart{part}, s);
   return e != hipSuccess ? e : launch_join_parts(part, out, true, g.splits, (long long)g.M * g.N, s);
 }
 
@@ -82,7 +89,7 @@ hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStrea
 
 size_t gated_part_bytes(int T, int d, int d_ff, int segments) {
   if (segments == 1 && T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff);
-  const int s = product_splits(T, d, segments * ((d_ff + kGemmStep - 1) / kGemmStep));
+  const int s = split_shape(T, d, d_ff, segments).splits;
   return s > 1 ? (size_t)s * T * d * sizeof(float) : 0;
 }
 
@@ -94,7 +101,7 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
   up.M = T, up.N = L.d_ff, up.K = L.d, up.lda = up.ldb = 2u * L.d;
   up.segments = up.products = up.splits = 1;
   const hipError_t e = with_activation(L.act, [&](auto act) {
-    return launch_product<true, true, true, false>(up, StoreGated<decltype(act)::value>{kept}, s);
+    return launch_product<true, true, true, false>(up, product_shape(T, 2 * L.d_ff, k_steps(L.d), 1, 1).tile, StoreGated<decltype(act)::value>{kept}, s);
   });
   if (e != hipSuccess) return e;
   GemmArgs down{};
@@ -114,7 +121,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
     a.segments = a.products = a.splits = 1;
     e = with_activation(L.act, [&](auto act) {
-      return launch_product<true, true, false, false>(a, StoreGateSlopes<decltype(act)::value>{kept, dg, du}, s);
+      return launch_product<true, true, false, false>(a, product_shape(T, L.d_ff, k_steps(L.d), 1, 1).tile, StoreGateSlopes<decltype(act)::value>{kept, dg, du}, s);
     });
     if (e != hipSuccess) return e;
   }
@@ -129,7 +136,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
     w.segments = w.splits = 1;
-    e = launch_product<false, false, false, false>(w, out, s);
+    e = launch_product<false, false, false, false>(w, product_shape(L.d_ff, L.d, k_steps(T), w.products, 1).tile, out, s);
     if (e != hipSuccess) return e;
   }
   if (dx) {

@@ -640,7 +640,8 @@ hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
     g.a_scales = reinterpret_cast<const uint8_t*>(padded);
     g.b_scales = reinterpret_cast<const uint8_t*>(padded + (size_t)p.T * words);
   }
-  return launch_product<true, true, false, true>(g, StoreProduct{p.y, p.y_bf16}, s);
+  const int tile = product_shape(p.T, p.rows, (p.cols + 127) / 128, 1, 1).tile;
+  return launch_product<true, true, false, true>(g, tile, StoreProduct{p.y, p.y_bf16}, s);
 }
 
 }  // namespace hire
