@@ -18,16 +18,31 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 // behind dy took 740 us instead of the 200 of its arithmetic (4096 tokens of d = 2048, 16384 units).
 constexpr int kRowFloats = 68;  // 64 columns and a gap that moves the rows over the banks
 
-// f(row m, column n of the first of eight, values): values[8] of a block column, or [2][8] of both (PAIRED).
-template <bool PAIRED, int MB, int NB, typename F>
-__device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, F f) {
+// f(row m, column n of the first of eight, values, fetched): values[8] of a block column, or [2][8] of both (PAIRED).
+// fetch(m, n): what an epilogue reads from memory for these eight, asked for a block of 32 rows ahead; for rows and columns that
+// are not there at the last ones.
+struct NoFetch {
+  __device__ __forceinline__ int operator()(int, int) const { return 0; }
+};
+template <bool PAIRED, int MB, int NB, typename Fetch, typename F>
+__device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, Fetch fetch, F f) {
   static_assert(NB == 2, "64 columns");
   const int lane = lane_id();
   float* tile = reinterpret_cast<float*>(smem) + wave_id() * 32 * kRowFloats;
-  constexpr int kLanes = PAIRED ? 4 : 8;  // lanes of a row
-  const int col = lane % kLanes * 8;
+  constexpr int kLanes = PAIRED ? 4 : 8, kPasses = 32 * kLanes / 64;  // lanes of a row
+  const int col = lane % kLanes * 8, row = lane / kLanes;
+  using Fetched = decltype(fetch(0, 0));
+  Fetched here[kPasses], ahead[kPasses];
+  auto request = [&](int i, Fetched (&to)[kPasses]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < kPasses; ++r) to[r] = fetch(min(m0 + 32 * i + r * (64 / kLanes) + row, M - 1), min(n0 + col, N - 8));
+  };
+  request(0, ahead);
 #pragma unroll
   for (int i = 0; i < MB; ++i) {
+#pragma unroll
+    for (int r = 0; r < kPasses; ++r) here[r] = ahead[r];
+    if (i + 1 < MB) request(i + 1, ahead);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's own reads of the block before
 #pragma unroll
     for (int j = 0; j < NB; ++j)
@@ -37,15 +52,15 @@ __device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* sme
             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += 64 / kLanes) {
-      const int r = r0 + lane / kLanes, m = m0 + 32 * i + r, n = n0 + col;
+    for (int pass = 0; pass < kPasses; ++pass) {
+      const int r = pass * (64 / kLanes) + row, m = m0 + 32 * i + r, n = n0 + col;
       float v[PAIRED ? 2 : 1][8];
 #pragma unroll
       for (int j = 0; j < (PAIRED ? 2 : 1); ++j) {
         *reinterpret_cast<float4*>(&v[j][0]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col);
         *reinterpret_cast<float4*>(&v[j][4]) = *reinterpret_cast<const float4*>(tile + r * kRowFloats + 32 * j + col + 4);
       }
-      if (m < M && n < N) f(m, n, v);
+      if (m < M && n < N) f(m, n, v, here[pass]);
     }
   }
 }
@@ -56,7 +71,7 @@ struct StorePart {
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int,
                                         int split) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
       float4* to = reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n);
       to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
       to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);

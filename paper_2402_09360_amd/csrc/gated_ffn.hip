@@ -9,7 +9,7 @@ struct StoreBf16 {
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int product,
                                         int) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
       *reinterpret_cast<uint4*>(c[product] + (size_t)m * N + n) = pack8(v[0]);
     });
   }
@@ -21,7 +21,7 @@ struct StoreGated {
   GatedKept kept;  // g null: h only
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
-    for_rows<true>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[2][8]) {
+    for_rows<true>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[2][8], int) {
       const size_t at = (size_t)m * N + n;
       float hv[8], slope;
 #pragma unroll
@@ -50,11 +50,18 @@ struct StoreGateSlopes {
   uint16_t *dg, *du;
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+    struct Planes {
+      uint4 g, u, low;
+    };
+    auto fetch = [&](int m, int n) {
+      const size_t at = (size_t)m * N + n;
+      return Planes{*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
+                    *reinterpret_cast<const uint4*>(kept.low + at)};
+    };
+    for_rows<false>(acc, smem, m0, n0, M, N, fetch, [&](int m, int n, const float (&v)[1][8], const Planes& k) {
       const size_t at = (size_t)m * N + n;
       float gv[8], uv[8], dgv[8], duv[8];
-      unpack_kept(*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
-                  *reinterpret_cast<const uint4*>(kept.low + at), gv, uv);
+      unpack_kept(k.g, k.u, k.low, gv, uv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float slope;

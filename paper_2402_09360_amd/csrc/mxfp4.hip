@@ -469,7 +469,7 @@ struct StoreProduct {
   int bf16;
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, [&](int m, int n, const float (&v)[1][8]) {
+    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
       const size_t at = (size_t)m * N + n;
       if (N % 8 != 0) {
 #pragma unroll
