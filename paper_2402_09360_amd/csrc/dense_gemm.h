@@ -33,11 +33,6 @@ __device__ __forceinline__ void gemm_load_at(const void* address, uint32_t lds) 
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(address), "s"(lds) : "memory", "m0");
 }
 
-// The same with four bytes per lane.
-__device__ __forceinline__ void gemm_load_words(const char* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
-}
-
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __bf16 v[2] = {(__bf16)lo, (__bf16)hi};  // nearest even
   uint32_t u;
@@ -142,7 +137,7 @@ struct GemmArgs {
   int products;      // > 1: so many products of one shape
   int splits;        // parts of k, whose sums the epilogue gets apart
   // microscaled operands only (a[0], b[0]: 4-bit codes, K in quarters of a column): scale bytes [M, scale_ld], [N, scale_ld],
-  // scale_ld a multiple of 4 (bytes behind the last block: 127)
+  // scale_ld a multiple of 16 (bytes behind the last block: 127)
   const uint8_t *a_scales, *b_scales;
   uint32_t scale_ld;
 };
@@ -176,9 +171,10 @@ __device__ __forceinline__ void gemm_barrier() {
 // in front of which every wave's reads of s - 1 were done.
 // An epilogue gets a wave's sums: acc[i][j], rows m of block i at lane % 32, columns n of block j: register r is column
 // 8 (r / 4) + 4 (lane / 32) + r % 4.
-// MX: microscaled operands.  A stage's 64 bytes of a row are 128 columns, four blocks; the row's four scale bytes travel beside
-// them, one word per row of both tiles.  A lane's sixteen bytes of a fragment are one block, whose scale byte the matrix
-// instruction picks from the row's word, shifted by a byte in the upper half of the wave.
+// MX: microscaled operands.  A stage's 64 bytes of a row are 128 columns, four blocks; every fourth stage brings the scale bytes
+// of four, sixteen for each row of both tiles (a word per row and stage would touch as many lines as the codes do).  A lane's sixteen
+// bytes of a fragment are one block, whose scale byte the matrix instruction picks from the row's word, shifted by a byte in the
+// upper half of the wave.
 // TILE 128, where there are too few tiles of 256 for the chip: four waves of 64 x 64 in one group; two workgroups of a compute unit
 // fill each other's waits.
 template <int TILE, bool AK, bool BK, bool PAIR, bool MX, class Epilogue>
@@ -189,9 +185,10 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
   using TA = GemmTile<TILE, kWaves, AK, false>;
   using TB = GemmTile<TILE, kWaves, BK, PAIR>;
   static_assert(!MX || (AK && BK && !PAIR), "rows of codes");
-  constexpr int kCodes = TA::kBytes + TB::kBytes, kStage = kCodes + (MX ? 2 * TILE * 4 : 0);
-  constexpr int kYounger = (kGemmStages - 2) * (TA::kLoads + TB::kLoads + (MX ? 1 : 0));
-  __shared__ __align__(1024) char smem[kGemmStages * kStage];
+  constexpr int kCodes = TA::kBytes + TB::kBytes, kScales = MX ? 2 * TILE * 16 : 0, kStage = kCodes;
+  // loads of the two younger stages; with scale bytes among them the wait is for one of those loads too
+  constexpr int kYounger = (kGemmStages - 2) * (TA::kLoads + TB::kLoads);
+  __shared__ __align__(1024) char smem[kGemmStages * kStage + 2 * kScales];
 
   const int n_tile = PAIR ? TILE / 2 : TILE;
   const int tiles_m = (g.M + TILE - 1) / TILE, tiles_n = (g.N + n_tile - 1) / n_tile, tiles = tiles_m * tiles_n;
@@ -216,7 +213,7 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
   if constexpr (MX) {
     const bool of_a = wave < kWaves / 2;
     const int row0 = of_a ? m0 : n0, last = (of_a ? g.M : g.N) - 1 - row0;
-    scales = reinterpret_cast<const char*>(of_a ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld + 4 * (size_t)s0;
+    scales = reinterpret_cast<const char*>(of_a ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld;
     scale_off = (uint32_t)min(wave % (kWaves / 2) * 64 + lane_id(), last) * g.scale_ld;
   }
   // the next stage to request: its place, addresses and what is left of its segment of k
@@ -232,12 +229,14 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   auto request = [&]() {
     const uint32_t lds = lds0 + (uint32_t)place * kStage;
+    if constexpr (MX) {
+      if (requested % 4 == 0) {
+        gemm_load(scales, scale_off, lds0 + kGemmStages * kStage + (uint32_t)(requested / 4 % 2) * kScales + wave * 1024);
+        scales += 16;
+      }
+    }
     ta.request(pa, nullptr, left, lds, wave);
     tb.request(pb, pb2, left, lds + TA::kBytes, wave);
-    if constexpr (MX) {
-      gemm_load_words(scales, scale_off, lds + kCodes + wave * 256);
-      scales += 4;
-    }
     place = place + 1 == kGemmStages ? 0 : place + 1;
     left -= kGemmStep;
     pa += AK ? 2 * kGemmStep : (size_t)kGemmStep * g.lda;
@@ -271,12 +270,13 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     uint32_t xa[kMB], xb[kNB];  // MX: bytes 0 and 2 are the scales of this lane's blocks
     if constexpr (MX) {
-      const uint32_t* words = reinterpret_cast<const uint32_t*>(sa + kCodes) + (lane_id() & 31);
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(smem + kGemmStages * kStage + (s / 4 % 2) * kScales) +
+                              4 * (lane_id() & 31) + s % 4;
       const int shift = lane_id() >> 5 << 3;
 #pragma unroll
-      for (int i = 0; i < kMB; ++i) xa[i] = words[wm + 32 * i] >> shift;
+      for (int i = 0; i < kMB; ++i) xa[i] = words[4 * (wm + 32 * i)] >> shift;
 #pragma unroll
-      for (int j = 0; j < kNB; ++j) xb[j] = words[TILE + wn + 32 * j] >> shift;
+      for (int j = 0; j < kNB; ++j) xb[j] = words[4 * (TILE + wn + 32 * j)] >> shift;
     }
     __builtin_amdgcn_sched_barrier(0);
     if (requested < n) {

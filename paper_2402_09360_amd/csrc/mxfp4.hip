@@ -491,8 +491,8 @@ struct StoreProduct {
   }
 };
 
-// Scale bytes in rows of whole words, 127 behind the last block: what the product reads where the columns are no multiple of
-// 128 (or the caller's bytes start between words).
+// Scale bytes in rows of whole sixteens, 127 behind the last block: what the product reads where the columns are no multiple of
+// 512 (or the caller's bytes start elsewhere).
 __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t* __restrict__ scales, long long rows, int blocks, int words,
                                                     uint32_t* __restrict__ out) {
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (long long)gridDim.x * 256) {
@@ -608,20 +608,20 @@ hipError_t launch_unpack_mxfp4(const uint8_t* codes, const uint8_t* scales, int 
 
 namespace {
 bool mx_pads_scales(const MxProduct& p) {
-  return p.cols % 128 != 0 || reinterpret_cast<uintptr_t>(p.x_scales) % 4 != 0 || reinterpret_cast<uintptr_t>(p.scales) % 4 != 0;
+  return p.cols % 512 != 0 || reinterpret_cast<uintptr_t>(p.x_scales) % 16 != 0 || reinterpret_cast<uintptr_t>(p.scales) % 16 != 0;
 }
 }  // namespace
 
 // Room for the parts of few tokens' sums, or for the padded scale bytes, whether this call's pointers need them or not.
 size_t mx_workspace_bytes(int T, int rows, int cols) {
-  if (T > kMxFewTokens) return ((size_t)T + rows) * ((cols / kMxBlock + 3) / 4) * 4;
+  if (T > kMxFewTokens) return ((size_t)T + rows) * ((cols / kMxBlock + 15) / 16) * 16;
   const int splits = few_splits(T, rows, cols);
   return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0;
 }
 
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
   if (p.T <= kMxFewTokens) return p.x_scales ? launch_few_tokens<true>(p, s) : launch_few_tokens<false>(p, s);
-  const int blocks = p.cols / kMxBlock, words = (blocks + 3) / 4;
+  const int blocks = p.cols / kMxBlock, words = (blocks + 15) / 16 * 4;
   GemmArgs g{};
   g.a[0] = p.x, g.b[0] = p.codes;
   g.M = p.T, g.N = p.rows, g.K = p.cols / 4, g.lda = g.ldb = (uint32_t)p.cols / 2;
