@@ -462,7 +462,7 @@ __global__ __launch_bounds__(64 * RW * KW) void k_mx_shared(const uint8_t* __res
     }
 }
 
-// ---- many tokens, packed ----------------------------------------------------------
+// ---- packed tokens in tiles ----------------------------------------------------------
 // y's rows out of the sums: whole vectors where the row length admits them.
 struct StoreProduct {
   void* y;
@@ -612,15 +612,29 @@ bool mx_pads_scales(const MxProduct& p) {
 }
 }  // namespace
 
-// Room for the parts of few tokens' sums, or for the padded scale bytes, whether this call's pointers need them or not.
+namespace {
+// Packed tokens as tiles of a dense product: always from 65 on, and where the rows are many enough for tiles of 128 of them; a few
+// tokens' tiles are mostly empty, but the tokens then come to LDS once for 128 rows.  us with the few tokens' kernel / as tiles,
+// 2048 columns: 256000 rows, 17 tokens 77 / 71, 64 128 / 79; 16384, 17 8.7 / 9.7, 33 10.2 / 9.9, 64 13.0 / 10.5; 1000 of 8192, 64
+// 11.1 / 27.4.
+bool mx_tiles(int T, int rows) {
+  return T > kMxFewTokens || (T > 32 && rows >= 16384) || (T > 8 && rows >= 65536);
+}
+size_t mx_padded_bytes(int T, int rows, int cols) { return ((size_t)T + rows) * ((cols / kMxBlock + 15) / 16) * 16; }
+}  // namespace
+
+// Room for the parts of few tokens' sums and for the padded scale bytes of tiles, whichever the call needs.
 size_t mx_workspace_bytes(int T, int rows, int cols) {
-  if (T > kMxFewTokens) return ((size_t)T + rows) * ((cols / kMxBlock + 15) / 16) * 16;
+  const size_t padded = mx_tiles(T, rows) ? mx_padded_bytes(T, rows, cols) : 0;
+  if (T > kMxFewTokens) return padded;
   const int splits = few_splits(T, rows, cols);
-  return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0;
+  const size_t parts = splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0;
+  return parts > padded ? parts : padded;
 }
 
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
-  if (p.T <= kMxFewTokens) return p.x_scales ? launch_few_tokens<true>(p, s) : launch_few_tokens<false>(p, s);
+  if (!p.x_scales) return launch_few_tokens<false>(p, s);
+  if (!mx_tiles(p.T, p.rows)) return launch_few_tokens<true>(p, s);
   const int blocks = p.cols / kMxBlock, words = (blocks + 15) / 16 * 4;
   GemmArgs g{};
   g.a[0] = p.x, g.b[0] = p.codes;
