@@ -1,4 +1,5 @@
-// The dense gated FFN, forward, for up to 64 tokens: bound by reading the three matrices once (6 d d_ff bytes).  Tokens are the
+// The dense gated FFN for up to 64 tokens, forward, and backward but for the weights' gradients: bound by reading the three
+// matrices once (6 d d_ff bytes).  Tokens are the
 // small side of 16 x 16 x 32 matrix instructions, whose other operand comes straight from memory into registers.
 #include "gated.h"
 
@@ -11,29 +12,32 @@ namespace {
 // lane / 16) and of one token of each tile: which k meet in an instruction is the same for both, so any order of them will do.
 // Every workgroup starts at another step: rows are a power of two apart more often than not, and where all start with their first
 // columns the requests crowd on a few of the memory's channels (one token, d = 2048, 16384 units: 31.6 -> 24.7 us).
-template <int NT, int RU, int SLICES>
-__device__ __forceinline__ void up_products(const uint16_t* __restrict__ x, int T, const GatedLayer& L, int unit0, int slice,
-                                            f32x4v (&g)[RU][NT], f32x4v (&u)[RU][NT]) {
-  const int lane = lane_id(), q = lane >> 4, chunks = L.d / 8, steps = (chunks + 7) / 8;
+// MATRICES: 2, or 1 (the backward pass's product with the second layer's rows).
+template <int MATRICES, int NT, int RU, int SLICES>
+__device__ __forceinline__ void up_products(const uint16_t* __restrict__ x, int T, int d, int d_ff,
+                                            const uint16_t* const (&w)[MATRICES], int unit0, int slice,
+                                            f32x4v (&sums)[RU][MATRICES][NT]) {
+  const int lane = lane_id(), q = lane >> 4, chunks = d / 8, steps = (chunks + 7) / 8;
   const int turn = (int)((blockIdx.x * 5u) % (unsigned)steps);
-  const uint4 *pg[RU], *pu[RU], *px[NT];
+  const uint4 *pw[RU][MATRICES], *px[NT];
 #pragma unroll
-  for (int r = 0; r < RU; ++r) {
-    const size_t row = (size_t)min(unit0 + 16 * r + (lane & 15), L.d_ff - 1) * L.d;
-    pg[r] = reinterpret_cast<const uint4*>(L.wg + row);
-    pu[r] = reinterpret_cast<const uint4*>(L.wu + row);
-  }
+  for (int r = 0; r < RU; ++r)
 #pragma unroll
-  for (int t = 0; t < NT; ++t) px[t] = reinterpret_cast<const uint4*>(x + (size_t)min(16 * t + (lane & 15), T - 1) * L.d);
+    for (int m = 0; m < MATRICES; ++m)
+      pw[r][m] = reinterpret_cast<const uint4*>(w[m] + (size_t)min(unit0 + 16 * r + (lane & 15), d_ff - 1) * d);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) px[t] = reinterpret_cast<const uint4*>(x + (size_t)min(16 * t + (lane & 15), T - 1) * d);
   auto chunk_of = [&](int s) { return 8 * (s + turn < steps ? s + turn : s + turn - steps) + 2 * q; };
-  auto load = [&](int s, uint4 (&wv)[RU][4], uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
+  auto load = [&](int s, uint4 (&wv)[RU][MATRICES][2], uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
     const int c = chunk_of(s), a = min(c, chunks - 1), b = min(c + 1, chunks - 1);
 #pragma unroll
-    for (int r = 0; r < RU; ++r) wv[r][0] = pg[r][a], wv[r][1] = pg[r][b], wv[r][2] = pu[r][a], wv[r][3] = pu[r][b];
+    for (int r = 0; r < RU; ++r)
+#pragma unroll
+      for (int m = 0; m < MATRICES; ++m) wv[r][m][0] = pw[r][m][a], wv[r][m][1] = pw[r][m][b];
 #pragma unroll
     for (int t = 0; t < NT; ++t) xv[t][0] = px[t][a], xv[t][1] = px[t][b];
   };
-  auto multiply = [&](int s, const uint4 (&wv)[RU][4], const uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
+  auto multiply = [&](int s, const uint4 (&wv)[RU][MATRICES][2], const uint4 (&xv)[NT][2]) __attribute__((always_inline)) {
     const int c = chunk_of(s);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -49,23 +53,25 @@ __device__ __forceinline__ void up_products(const uint16_t* __restrict__ x, int 
       for (int t = 0; t < NT; ++t) xf[t] = masked(xv[t][e]);
 #pragma unroll
       for (int r = 0; r < RU; ++r) {
-        const bf16x8v wgv = masked(wv[r][e]), wuv = masked(wv[r][2 + e]);
+        bf16x8v wf[MATRICES];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          g[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wgv, xf[t], g[r][t], 0, 0, 0);
-          u[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wuv, xf[t], u[r][t], 0, 0, 0);
-        }
+        for (int m = 0; m < MATRICES; ++m) wf[m] = masked(wv[r][m][e]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int m = 0; m < MATRICES; ++m)
+            sums[r][m][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[m], xf[t], sums[r][m][t], 0, 0, 0);
       }
     }
   };
-  uint4 wa[RU][4], xa[NT][2];
+  uint4 wa[RU][MATRICES][2], xa[NT][2];
   if constexpr (RU > 1) {  // the sums leave room for one step; the waves of a SIMD overlap theirs
     for (int s = slice; s < steps; s += SLICES) {
       load(s, wa, xa);
       multiply(s, wa, xa);
     }
   } else {
-    uint4 wb[RU][4], xb[NT][2];
+    uint4 wb[RU][MATRICES][2], xb[NT][2];
     int s = slice;
     if (s >= steps) return;
     load(s, wa, xa);
@@ -79,23 +85,25 @@ __device__ __forceinline__ void up_products(const uint16_t* __restrict__ x, int 
   }
 }
 
-// Adds the slices' sums in their order; red: LDS, [groups of units][SLICES][2 NT 256].  unit (of the group's sixteen) and token
-// of value i; f(unit, token, g, u).
-template <int NT, int SLICES, typename F>
+// Adds the slices' sums in their order; red: LDS, [SLICES][MATRICES NT 256] of sixteen units.  f(unit, token, sums) for value i.
+template <int MATRICES, int NT, int SLICES, typename F>
 __device__ __forceinline__ void join_slices(const float* red, int i, F f) {
   const int unit = i & 15, token = i >> 4, at = (token >> 4) * 256 + ((unit >> 2) * 16 + (token & 15)) * 4 + (unit & 3);
-  float g = red[at], u = red[NT * 256 + at];
+  float v[MATRICES];
 #pragma unroll
-  for (int s = 1; s < SLICES; ++s) g += red[s * 2 * NT * 256 + at], u += red[(s * 2 + 1) * NT * 256 + at];
-  f(unit, token, g, u);
+  for (int m = 0; m < MATRICES; ++m) v[m] = red[m * NT * 256 + at];
+#pragma unroll
+  for (int s = 1; s < SLICES; ++s)
+#pragma unroll
+    for (int m = 0; m < MATRICES; ++m) v[m] += red[(s * MATRICES + m) * NT * 256 + at];
+  f(unit, token, v);
 }
-template <int NT>
-__device__ __forceinline__ void leave_slice(float* red, const f32x4v (&g)[NT], const f32x4v (&u)[NT]) {
+template <int MATRICES, int NT>
+__device__ __forceinline__ void leave_slice(float* red, const f32x4v (&sums)[MATRICES][NT]) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    *reinterpret_cast<f32x4v*>(red + (t * 64 + lane_id()) * 4) = g[t];
-    *reinterpret_cast<f32x4v*>(red + ((NT + t) * 64 + lane_id()) * 4) = u[t];
-  }
+  for (int m = 0; m < MATRICES; ++m)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4v*>(red + ((m * NT + t) * 64 + lane_id()) * 4) = sums[m][t];
 }
 __device__ __forceinline__ void keep_gated(const GatedKept& kept, size_t at, float g, float u) {
   kept.g[at] = (uint16_t)(__float_as_uint(g) >> 16);
@@ -109,22 +117,52 @@ template <int ACT, int NT, int RU>
 __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const uint16_t* __restrict__ x, int T, GatedKept kept) {
   __shared__ float red[kUpWaves * 2 * NT * 256];
   const int unit0 = blockIdx.x * 16 * RU;
-  f32x4v g[RU][NT] = {}, u[RU][NT] = {};
-  up_products<NT, RU, kUpWaves>(x, T, L, unit0, wave_id(), g, u);
+  f32x4v sums[RU][2][NT] = {};
+  up_products<2, NT, RU, kUpWaves>(x, T, L.d, L.d_ff, {L.wg, L.wu}, unit0, wave_id(), sums);
 #pragma unroll
   for (int r = 0; r < RU; ++r) {
     if (r > 0) __syncthreads();
-    leave_slice<NT>(red + wave_id() * 2 * NT * 256, g[r], u[r]);
+    leave_slice<2, NT>(red + wave_id() * 2 * NT * 256, sums[r]);
     __syncthreads();
     for (int i = threadIdx.x; i < NT * 256; i += 64 * kUpWaves)
-      join_slices<NT, kUpWaves>(red, i, [&](int unit, int token, float gv, float uv) {
+      join_slices<2, NT, kUpWaves>(red, i, [&](int unit, int token, const float (&v)[2]) {
         const int f = unit0 + 16 * r + unit;
         if (token >= T || f >= L.d_ff) return;
         const size_t at = (size_t)token * L.d_ff + f;
         float slope;
-        const __bf16 h = (__bf16)(activation<ACT>(gv, &slope) * uv);
+        const __bf16 h = (__bf16)(activation<ACT>(v[0], &slope) * v[1]);
         __builtin_memcpy(kept.h + at, &h, 2);
-        if (kept.g) keep_gated(kept, at, gv, uv);
+        if (kept.g) keep_gated(kept, at, v[0], v[1]);
+      });
+  }
+}
+
+// The backward pass's first product: dh of the units, and from it and what was kept dg and du.
+template <int ACT, int NT, int RU>
+__global__ __launch_bounds__(64 * kUpWaves) void k_gated_slopes(GatedLayer L, const uint16_t* __restrict__ dy, int T, GatedKept kept,
+                                                                uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
+  __shared__ float red[kUpWaves * NT * 256];
+  const int unit0 = blockIdx.x * 16 * RU;
+  f32x4v sums[RU][1][NT] = {};
+  up_products<1, NT, RU, kUpWaves>(dy, T, L.d, L.d_ff, {L.w2u}, unit0, wave_id(), sums);
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    if (r > 0) __syncthreads();
+    leave_slice<1, NT>(red + wave_id() * NT * 256, sums[r]);
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 256; i += 64 * kUpWaves)
+      join_slices<1, NT, kUpWaves>(red, i, [&](int unit, int token, const float (&dh)[1]) {
+        const int f = unit0 + 16 * r + unit;
+        if (token >= T || f >= L.d_ff) return;
+        const size_t at = (size_t)token * L.d_ff + f;
+        const uint32_t low = kept.low[at];
+        const float gv = __uint_as_float((uint32_t)kept.g[at] << 16 | (low & 0xFFu) << 8);
+        const float uv = __uint_as_float((uint32_t)kept.u[at] << 16 | (low & 0xFF00u));
+        float slope;
+        const float a = activation<ACT>(gv, &slope);
+        const __bf16 dgv = (__bf16)(dh[0] * uv * slope), duv = (__bf16)(dh[0] * a);
+        __builtin_memcpy(dg + at, &dgv, 2);
+        __builtin_memcpy(du + at, &duv, 2);
       });
   }
 }
@@ -160,27 +198,33 @@ __device__ __forceinline__ void mask_rows(int row0, int end, uint4 (&rows)[8]) {
 
 constexpr int kDownWaves = 8;
 
-// Columns 128 blockIdx.x ..., rows of part blockIdx.y: the waves take blocks of 32 rows in turn.  The parts' sums are joined by
-// k_join_parts; one part only: y itself.
+// Columns 128 blockIdx.x ..., rows of part blockIdx.y: the waves take blocks of 32 rows in turn, of the second pair of matrix and
+// values behind those of the first (dx; a pair only: y).  The parts' sums are joined by k_join_parts; one part only: the result
+// itself.
+struct DownPairs {
+  const uint16_t *w[2], *h[2];
+  int pairs;
+};
 template <int NT>
-__global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(const uint16_t* __restrict__ w2, const uint16_t* __restrict__ h, int T,
-                                                                int d, int d_ff, float* __restrict__ part,
+__global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(DownPairs from, int T, int d, int d_ff, float* __restrict__ part,
                                                                 uint16_t* __restrict__ y) {
   __shared__ float red[kDownWaves * 2048];
-  const int lane = lane_id(), wave = wave_id(), parts = gridDim.y, blocks = (d_ff + 31) / 32;
+  const int lane = lane_id(), wave = wave_id(), parts = gridDim.y, each = (d_ff + 31) / 32, blocks = each * from.pairs;
   const int b0 = (int)((long long)blocks * blockIdx.y / parts), b1 = (int)((long long)blocks * (blockIdx.y + 1) / parts);
   const int chunk = min((int)blockIdx.x * 16 + (lane & 15), d / 8 - 1);
-  const uint16_t* ph[NT];
+  size_t token[NT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) ph[t] = h + (size_t)min(16 * t + (lane & 15), T - 1) * d_ff;
+  for (int t = 0; t < NT; ++t) token[t] = (size_t)min(16 * t + (lane & 15), T - 1) * d_ff;
   f32x4v acc[NT][8] = {};
-  auto load = [&](int b, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
-    load_rows(w2, d, chunk, 32 * b, d_ff, rows);
-    const int at = min(32 * b + 8 * (lane >> 4), d_ff - 8);
+  auto load = [&](int block, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
+    const int pair = block >= each ? 1 : 0, b = block - pair * each;  // uniform
+    load_rows(from.w[pair], d, chunk, 32 * b, d_ff, rows);
+    const uint16_t* h = from.h[pair] + min(32 * b + 8 * (lane >> 4), d_ff - 8);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) hv[t] = *reinterpret_cast<const uint4*>(ph[t] + at);
+    for (int t = 0; t < NT; ++t) hv[t] = *reinterpret_cast<const uint4*>(h + token[t]);
   };
-  auto multiply = [&](int b, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
+  auto multiply = [&](int block, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
+    const int b = block >= each ? block - each : block;
     if (32 * b + 32 > d_ff) {  // uniform; d_ff is a multiple of 8, so a lane's eight rows are there or not as a whole
       mask_rows(32 * b, d_ff, rows);
       if (32 * b + 8 * (lane >> 4) >= d_ff) {
@@ -247,9 +291,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(const uint16_t* 
   }
 }
 
-// Parts of the second layer's rows: about 512 workgroups, of at least one block of 32 rows per wave.
-int down_parts(int d, int d_ff) {
-  const int columns = (d + 127) / 128, most = (d_ff + 32 * kDownWaves - 1) / (32 * kDownWaves);
+// Parts of the rows: about 512 workgroups, of at least one block of 32 rows per wave.
+int down_parts(int d, int rows) {
+  const int columns = (d + 127) / 128, most = (rows + 32 * kDownWaves - 1) / (32 * kDownWaves);
   int parts = 512 / columns;
   parts = parts < 1 ? 1 : (parts > 16 ? 16 : parts);
   return parts < most ? parts : most;
@@ -267,26 +311,26 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, cons
   __shared__ __align__(16) __bf16 hidden[16 * kBlocks * 32];
   const int lane = lane_id(), wave = wave_id(), unit0 = blockIdx.x * kUnits, end = min(unit0 + kUnits, L.d_ff);
   const int group = wave % GROUPS, columns = (L.d + 127) / 128;
-  f32x4v g[1][1] = {}, u[1][1] = {};
-  up_products<1, 1, kSlices>(x, T, L, unit0 + 16 * group, wave / GROUPS, g, u);
+  f32x4v products[1][2][1] = {};
+  up_products<2, 1, 1, kSlices>(x, T, L.d, L.d_ff, {L.wg, L.wu}, unit0 + 16 * group, wave / GROUPS, products);
   auto chunk_of = [&](int block) { return min(16 * block + (lane & 15), L.d / 8 - 1); };
   uint4 rows[kBlocks][8];
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b) load_rows(L.w2u, L.d, chunk_of(min(wave, columns - 1)), unit0 + 32 * b, end, rows[b]);
-  leave_slice<1>(red + (group * kSlices + wave / GROUPS) * 512, g[0], u[0]);
+  leave_slice<2, 1>(red + (group * kSlices + wave / GROUPS) * 512, products[0]);
   for (int i = threadIdx.x; i < 16 * kBlocks * 32; i += 64 * kOneWaves) hidden[i] = (__bf16)0.0f;
   __syncthreads();
   for (int i = threadIdx.x; i < GROUPS * 256; i += 64 * kOneWaves)
-    join_slices<1, kSlices>(red + i / 256 * kSlices * 512, i % 256, [&](int unit, int token, float gv, float uv) {
+    join_slices<2, 1, kSlices>(red + i / 256 * kSlices * 512, i % 256, [&](int unit, int token, const float (&v)[2]) {
       const int in = i / 256 * 16 + unit;
       if (token >= T || unit0 + in >= L.d_ff) return;
       float slope;
-      const __bf16 h = (__bf16)(activation<ACT>(gv, &slope) * uv);
+      const __bf16 h = (__bf16)(activation<ACT>(v[0], &slope) * v[1]);
       hidden[token * kBlocks * 32 + in] = h;
       if (kept.g) {
         const size_t at = (size_t)token * L.d_ff + unit0 + in;
         __builtin_memcpy(kept.h + at, &h, 2);
-        keep_gated(kept, at, gv, uv);
+        keep_gated(kept, at, v[0], v[1]);
       }
     });
   __syncthreads();
@@ -357,18 +401,46 @@ hipError_t launch_one(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y
                          : launch(&k_join_units, dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, part, y, parts, quads);
 }
 
+// out = the sum over the pairs' rows, in parts where they are many.
+template <int NT>
+hipError_t launch_down(const DownPairs& from, int T, int d, int d_ff, uint16_t* out, float* part, hipStream_t s) {
+  const int parts = down_parts(d, from.pairs * d_ff);
+  const hipError_t e = launch(&k_gated_down<NT>, dim3((unsigned)((d + 127) / 128), (unsigned)parts), dim3(64 * kDownWaves), 0, s, from, T,
+                              d, d_ff, part, out);
+  if (e != hipSuccess || parts == 1) return e;
+  return launch_join_parts(part, out, true, parts, (long long)T * d, s);
+}
+
 template <int NT, int RU>
 hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
-  hipError_t e = with_activation(L.act, [&](auto act) {
+  const hipError_t e = with_activation(L.act, [&](auto act) {
     return launch(&k_gated_up<decltype(act)::value, NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
                   dim3(64 * kUpWaves), 0, s, L, x, T, kept);
   });
-  if (e != hipSuccess) return e;
-  const int parts = down_parts(L.d, L.d_ff);
-  e = launch(&k_gated_down<NT>, dim3((unsigned)((L.d + 127) / 128), (unsigned)parts), dim3(64 * kDownWaves), 0, s, L.w2u, kept.h, T,
-             L.d, L.d_ff, part, y);
-  if (e != hipSuccess || parts == 1) return e;
-  return launch_join_parts(part, y, true, parts, (long long)T * L.d, s);
+  return e != hipSuccess ? e : launch_down<NT>(DownPairs{{L.w2u, nullptr}, {kept.h, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
+}
+
+template <int NT>
+hipError_t launch_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+                         hipStream_t s) {
+  const int groups = (L.d_ff + 15) / 16;
+  return with_activation(L.act, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if (groups >= 2 * 256)
+      return launch(&k_gated_slopes<ACT, NT, 2>, dim3((unsigned)((groups + 1) / 2)), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
+    return launch(&k_gated_slopes<ACT, NT, 1>, dim3((unsigned)groups), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
+  });
+}
+
+// f with the number of tiles of sixteen tokens as a type.
+template <typename F>
+hipError_t with_tiles(int T, F f) {
+  switch ((T + 15) / 16) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 3: return f(std::integral_constant<int, 3>{});
+    default: return f(std::integral_constant<int, 4>{});
+  }
 }
 
 // Units of a workgroup of the first layer, in sixteens.  More of them share what is read of the tokens, which comes from the L2
@@ -385,9 +457,9 @@ hipError_t launch_few_by_width(const GatedLayer& L, const uint16_t* x, int T, ui
 
 }  // namespace
 
-size_t gated_few_part_bytes(int T, int d, int d_ff) {
-  if (one_kernel(T, d, d_ff)) return (size_t)one_parts(d_ff) * T * d * sizeof(float);
-  const int parts = down_parts(d, d_ff);
+size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs) {
+  if (pairs == 1 && one_kernel(T, d, d_ff)) return (size_t)one_parts(d_ff) * T * d * sizeof(float);
+  const int parts = down_parts(d, pairs * d_ff);
   return parts > 1 ? (size_t)parts * T * d * sizeof(float) : 0;
 }
 
@@ -398,11 +470,22 @@ hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint1
     if (groups == 4) return launch_one<4, 8>(L, x, T, y, kept, part, s);
     return groups == 2 ? launch_one<2, 8>(L, x, T, y, kept, part, s) : launch_one<1, 16>(L, x, T, y, kept, part, s);
   }
-  const int tiles = (T + 15) / 16;
-  if (tiles == 1) return launch_few_by_width<1, 2>(L, x, T, y, kept, part, s);
-  if (tiles == 2) return launch_few_by_width<2, 2>(L, x, T, y, kept, part, s);
-  if (tiles == 3) return launch_few_by_width<3, 4>(L, x, T, y, kept, part, s);
-  return launch_few_by_width<4, 4>(L, x, T, y, kept, part, s);
+  return with_tiles(T, [&](auto tiles) {
+    constexpr int NT = decltype(tiles)::value;
+    return launch_few_by_width<NT, NT <= 2 ? 2 : 4>(L, x, T, y, kept, part, s);
+  });
+}
+
+hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+                                   hipStream_t s) {
+  return with_tiles(T, [&](auto tiles) { return launch_slopes<decltype(tiles)::value>(L, dy, T, kept, dg, du, s); });
+}
+
+hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
+                               hipStream_t s) {
+  return with_tiles(T, [&](auto tiles) {
+    return launch_down<decltype(tiles)::value>(DownPairs{{L.wg, L.wu}, {dg, du}, 2}, T, L.d, L.d_ff, dx, part, s);
+  });
 }
 
 }  // namespace hire

@@ -95,7 +95,7 @@ hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStrea
 }  // namespace
 
 size_t gated_part_bytes(int T, int d, int d_ff, int segments) {
-  if (segments == 1 && T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff);
+  if (T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff, segments);
   const int s = split_shape(T, d, d_ff, segments).splits;
   return s > 1 ? (size_t)s * T * d * sizeof(float) : 0;
 }
@@ -122,7 +122,11 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
                                  uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
                                  float* part, hipStream_t s) {
   hipError_t e = hipSuccess;
-  if (dx || dwg || dwu) {
+  const bool few = T <= kGatedFewTokens;
+  if (few && (dx || dwg || dwu)) {
+    e = launch_gated_few_slopes(L, dy, T, kept, dg, du, s);
+    if (e != hipSuccess) return e;
+  } else if (dx || dwg || dwu) {
     GemmArgs a{};
     a.a[0] = dy, a.b[0] = L.w2u;
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
@@ -146,6 +150,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     e = launch_product<false, false, false, false>(w, product_shape(L.d_ff, L.d, k_steps(T), w.products, 1).tile, out, s);
     if (e != hipSuccess) return e;
   }
+  if (dx && few) return launch_gated_few_dx(L, T, dg, du, dx, part, s);
   if (dx) {
     GemmArgs a{};
     a.a[0] = dg, a.a[1] = du, a.b[0] = L.wg, a.b[1] = L.wu;

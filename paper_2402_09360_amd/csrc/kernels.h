@@ -492,11 +492,15 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
                                  uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
                                  float* part, hipStream_t s);
 
-// ---- gated_few.hip: the forward pass of up to kGatedFewTokens tokens
+// ---- gated_few.hip: up to kGatedFewTokens tokens; the backward pass's dg and du, and dx from them
 constexpr int kGatedFewTokens = 64;
-size_t gated_few_part_bytes(int T, int d, int d_ff);
+size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs);  // pairs: 1 forward, 2 dx
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                             hipStream_t s);
+hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+                                   hipStream_t s);
+hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
+                               hipStream_t s);
 
 // ---- mxfp4.hip: microscaled 4-bit floating point ---------------------------------
 hipError_t launch_pack_mxfp4(const uint16_t* w, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s);
