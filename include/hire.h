@@ -285,8 +285,8 @@ typedef struct hire_gated_layer {
  * to bf16 between the two layers.  saved: hire_gated_ffn_saved_bytes(L, T) bytes, 256-byte aligned, that receive what
  * hire_gated_ffn_backward reads (opaque: h in bf16, g and u in 24 bits), or NULL where no backward pass follows; y does not
  * depend on it.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on invalid arguments, never 0 on valid ones),
- * 256-byte aligned; no initialisation needed, and hire_workspace_init does no harm.  x and y must not overlap.
- * HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
+ * 256-byte aligned; no initialisation needed, and hire_workspace_init does no harm.  Outputs overlap neither inputs nor
+ * each other, here and below.  HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
 size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T);
 size_t hire_gated_ffn_saved_bytes(const hire_gated_layer* L, int T);
 int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y, void* saved, void* workspace,

@@ -11,8 +11,8 @@ constexpr float kGelu = 1.5957691216057308f, kGeluCube = 0.044715f, kLog2E = 1.4
 template <int ACT>
 __device__ __forceinline__ float activation(float g, float* slope) {
   if constexpr (ACT == kActRelu) {
-    *slope = g > 0.0f ? 1.0f : 0.0f;
-    return g > 0.0f ? g : 0.0f;
+    *slope = g <= 0.0f ? 0.0f : 1.0f;  // a NaN stays one
+    return g <= 0.0f ? 0.0f : g;
   } else {
     const float z = ACT == kActSilu ? g : kGelu * (g + kGeluCube * g * g * g);
     const float dz = ACT == kActSilu ? 1.0f : kGelu * (1.0f + 3.0f * kGeluCube * g * g);
@@ -25,8 +25,8 @@ __device__ __forceinline__ float activation(float g, float* slope) {
 
 // What the forward call keeps for the backward one: planes of 16 bits per unit and token.  h is rounded to bf16 as the second
 // product reads it.  g and u keep 24 bits of their fp32 (15 of the significand), the upper 16 in planes of their own and the
-// lower 8 of both in a third (GatedKept): rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to dwg instead
-// of 0.0024 (0.0017 is the rounding of dwg itself).
+// lower 8 of both in a third (GatedKept): rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to
+// dwg instead of 0.0024 (0.0017 is the rounding of dwg itself).
 __device__ __forceinline__ uint32_t upper_pair(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }

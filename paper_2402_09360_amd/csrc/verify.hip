@@ -246,7 +246,8 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
 
 // Short lists (or a draft that was certain): a wave for every position takes its lists into registers before it is known which
 // positions are reached, so that everything is asked for at once; the wave of the position behind the accepted tokens then does
-// the rest alone.  Eight sequences of four drafted tokens with lists of 64: LISTS_US.
+// the rest alone.  Eight sequences of four drafted tokens with lists of 64: 5.9 us (12.6 by a workgroup
+// that takes one step after the other, as k_verify_lists does).
 constexpr int kShortEach = 4;                       // entries of a lane
 constexpr int kShortList = kShortEach * kWave;      // longest list
 constexpr int kShortWaves = 16;                     // most positions

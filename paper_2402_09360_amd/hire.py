@@ -546,6 +546,18 @@ def _tensor(t, dtype, shape, where):
     return t.data_ptr()
 
 
+def _room(workspace, where):
+    """Address and bytes of a workspace on the current device."""
+    if not workspace.is_contiguous() or workspace.get_device() != _current_device():
+        raise HireError(EINVAL, f"{where}: a contiguous workspace on the current device wanted, got one on {workspace.device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _on_device(device, what, where):
+    if device.index != _current_device():
+        raise HireError(EINVAL, f"{where}: {what} on the current device wanted, got {device}")
+
+
 ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2
 _ACTS = {"relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU}
 
@@ -555,11 +567,11 @@ class GatedLayer:
 
     def __init__(self, wg, wu, w2u, act="silu"):
         for t in (wg, wu, w2u):
-            if t.dim() != 2 or t.shape != wg.shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or not t.is_cuda:
-                raise HireError(EINVAL, "GatedLayer: contiguous bf16 [d_ff, d_model] device matrices")
+            if t.dim() != 2 or t.shape != wg.shape or t.dtype != torch.bfloat16 or not t.is_contiguous() or not t.is_cuda or t.device != wg.device:
+                raise HireError(EINVAL, "GatedLayer: contiguous bf16 [d_ff, d_model] matrices of one device")
         if act not in _ACTS:
             raise HireError(EINVAL, f"GatedLayer: act is one of {sorted(_ACTS)}")
-        self.wg, self.wu, self.w2u, self.act = wg, wu, w2u, act
+        self.wg, self.wu, self.w2u, self.act, self.device = wg, wu, w2u, act, wg.device
         self.d_ff, self.d_model = wg.shape
         self.c = _GatedLayer(self.d_model, self.d_ff, wg.data_ptr(), wu.data_ptr(), w2u.data_ptr(), _ACTS[act])
         self.ref = C.byref(self.c)
@@ -599,16 +611,18 @@ def hire_gated_ffn_step(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, w
                         stream=None) -> None:
     """Enqueue the dense gated FFN of x bf16 [T, d_model]."""
     where, bf16, T = "hire_gated_ffn_step", torch.bfloat16, x.shape[0]
+    _on_device(layer.device, "the layer", where)
     tokens = (T, layer.d_model)
     saved = None if out.saved is None else _tensor(out.saved, torch.uint8, (hire_gated_ffn_saved_bytes(layer, T),), where)
     _check(_lib.hire_gated_ffn_step(layer.ref, _tensor(x, bf16, tokens, where), T, _tensor(out.y, bf16, tokens, where), saved,
-                                    _ptr(workspace), workspace.numel(), _stream(stream)), where)
+                                    *_room(workspace, where), _stream(stream)), where)
 
 
 def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, dy: torch.Tensor,
                             grads: GatedGradients, workspace: torch.Tensor, stream=None) -> None:
     """Enqueue the gradients for dy bf16 [T, d_model]; `out` as the forward call with train=True left it."""
     where, bf16, T = "hire_gated_ffn_backward", torch.bfloat16, x.shape[0]
+    _on_device(layer.device, "the layer", where)
     tokens, weights = (T, layer.d_model), (layer.d_ff, layer.d_model)
     if out.saved is None:
         raise HireError(EINVAL, f"{where}: outputs made with train=True")
@@ -616,7 +630,7 @@ def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutput
     wanted = [None if t is None else _tensor(t, bf16, shape, where)
               for t, shape in ((grads.dx, tokens), (grads.dwg, weights), (grads.dwu, weights), (grads.dw2u, weights))]
     _check(_lib.hire_gated_ffn_backward(layer.ref, _tensor(x, bf16, tokens, where), T, saved, _tensor(dy, bf16, tokens, where),
-                                        *wanted, _ptr(workspace), workspace.numel(), _stream(stream)), where)
+                                        *wanted, *_room(workspace, where), _stream(stream)), where)
 
 
 F32, BF16 = 0, 1
@@ -643,8 +657,7 @@ class Mxfp4:
                    torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
 
     def _addresses(self, where):
-        if self.codes.get_device() != _current_device():
-            raise HireError(EINVAL, f"{where}: packed matrix on the current device wanted, got {self.codes.device}")
+        _on_device(self.codes.device, "a packed matrix", where)
         return self.codes.data_ptr(), self.scales.data_ptr()
 
 
@@ -687,7 +700,7 @@ def hire_mxfp4_product(x: Mxfp4, w: Mxfp4, y: torch.Tensor, workspace: torch.Ten
     if x.cols != w.cols:
         raise HireError(EINVAL, f"{where}: {x.cols} and {w.cols} columns")
     _check(_lib.hire_mxfp4_product(*x._addresses(where), x.rows, *w._addresses(where), w.rows, w.cols,
-                                   *_product_output(y, x.rows, w.rows, where), _ptr(workspace), workspace.numel(),
+                                   *_product_output(y, x.rows, w.rows, where), *_room(workspace, where),
                                    _stream(stream)), where)
 
 
@@ -695,7 +708,7 @@ def hire_mxfp4_product_bf16(x: torch.Tensor, w: Mxfp4, y: torch.Tensor, workspac
     """Enqueue y [T, rows] (float32 or bfloat16) = x w^T for x bf16 [T, cols], at most MAX_BATCH tokens."""
     where, T = "hire_mxfp4_product_bf16", x.shape[0]
     _check(_lib.hire_mxfp4_product_bf16(_tensor(x, torch.bfloat16, (T, w.cols), where), T, *w._addresses(where), w.rows, w.cols,
-                                        *_product_output(y, T, w.rows, where), _ptr(workspace), workspace.numel(),
+                                        *_product_output(y, T, w.rows, where), *_room(workspace, where),
                                         _stream(stream)), where)
 
 
@@ -747,8 +760,9 @@ def hire_verify_draft_workspace_bytes(drafts: Drafts) -> int:
 def hire_verify_draft(drafts: Drafts, out: DraftOutputs, workspace: torch.Tensor, stream=None) -> None:
     """Enqueue the verification: the accepted tokens and the one that follows, and how many were accepted."""
     where = "hire_verify_draft"
+    _on_device(drafts.device, "the drafts", where)
     _check(_lib.hire_verify_draft(drafts.ref, _tensor(out.tokens, torch.int32, (drafts.B, drafts.n + 1), where),
-                                  _tensor(out.accepted, torch.int32, (drafts.B,), where), _ptr(workspace), workspace.numel(),
+                                  _tensor(out.accepted, torch.int32, (drafts.B,), where), *_room(workspace, where),
                                   _stream(stream)), where)
 
 
