@@ -78,7 +78,7 @@ extern "C" {
 
 size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T) {
   if (check_gated(L, T) != HIRE_OK) return 0;
-  return hidden_bytes(L, T) + align_up(gated_part_bytes(T, L->d_model, L->d_ff, 1));
+  return hidden_bytes(L, T) + align_up(gated_forward_part_bytes(T, L->d_model, L->d_ff));
 }
 
 size_t hire_gated_ffn_saved_bytes(const hire_gated_layer* L, int T) {
@@ -99,7 +99,7 @@ int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y
 
 size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T) {
   if (check_gated(L, T) != HIRE_OK) return 0;
-  return 2 * hidden_bytes(L, T) + align_up(gated_part_bytes(T, L->d_model, L->d_ff, 2));
+  return 2 * hidden_bytes(L, T) + align_up(gated_backward_part_bytes(T, L->d_model, L->d_ff));
 }
 
 int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* saved, const void* dy, void* dx,

@@ -65,24 +65,51 @@ __device__ __forceinline__ void for_rows(const f32x16v (&acc)[MB][NB], char* sme
   }
 }
 
-// fp32 sums of one part of k; N a multiple of 8.
+// fp32 sums of one part of k; N a multiple of 8.  In order: products, parts, both matrices (PAIRED), rows.
+template <bool PAIRED>
 struct StorePart {
   float* part;
+  int splits;
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int,
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int product,
                                         int split) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
-      float4* to = reinterpret_cast<float4*>(part + ((size_t)split * M + m) * N + n);
-      to[0] = make_float4(v[0][0], v[0][1], v[0][2], v[0][3]);
-      to[1] = make_float4(v[0][4], v[0][5], v[0][6], v[0][7]);
+    constexpr int kMatrices = PAIRED ? 2 : 1;
+    float* mine = part + (size_t)(product * splits + split) * kMatrices * M * N;
+    for_rows<PAIRED>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[kMatrices][8], int) {
+#pragma unroll
+      for (int j = 0; j < kMatrices; ++j) {
+        float4* to = reinterpret_cast<float4*>(mine + ((size_t)j * M + m) * N + n);
+        to[0] = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
+        to[1] = make_float4(v[j][4], v[j][5], v[j][6], v[j][7]);
+      }
     });
   }
 };
+// Eight values of a plane, added over the parts in their order; `stride` values from part to part.
+__device__ __forceinline__ void join_eight(const float* part, int parts, size_t stride, float (&v)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(part)[0], b = reinterpret_cast<const float4*>(part)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  for (int r = 1; r < parts; ++r) {
+    const float4* p = reinterpret_cast<const float4*>(part + r * stride);
+    const float4 c = p[0], d = p[1];
+    v[0] += c.x, v[1] += c.y, v[2] += c.z, v[3] += c.w, v[4] += d.x, v[5] += d.y, v[6] += d.z, v[7] += d.w;
+  }
+}
+inline unsigned join_blocks(long long threads) {
+  const long long blocks = (threads + 255) / 256;
+  return (unsigned)(blocks < 4096 ? blocks : 4096);
+}
 
-// Sum of the parts in their order, rounded once to bf16 or left in fp32; values beyond whole fours one by one.
+// Sum of the parts in their order, rounded once to bf16 or left in fp32, of products blockIdx.y; values beyond whole fours
+// one by one.
+struct JoinOutputs {
+  void* out[3];
+};
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ part, void* __restrict__ out, int parts,
+__global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ part, JoinOutputs outputs, int parts,
                                                     long long values) {
+  void* out = outputs.out[blockIdx.y];
+  part += (size_t)blockIdx.y * parts * values;
   if (values % 4 != 0) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < values; i += (long long)gridDim.x * 256) {
       float s = part[i];
@@ -110,15 +137,22 @@ __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ pa
     }
   }
 }
+inline hipError_t launch_join_products(const float* part, const JoinOutputs& out, int products, bool bf16, int parts,
+                                       long long values, hipStream_t s) {
+  return launch(bf16 ? &k_join_parts<true> : &k_join_parts<false>, dim3(join_blocks(values / 4 + 1), (unsigned)products), dim3(256),
+                0, s, part, out, parts, values);
+}
 inline hipError_t launch_join_parts(const float* part, void* out, bool bf16, int parts, long long values, hipStream_t s) {
-  const long long blocks = (values / 4 + 255) / 256 + 1;
-  return launch(bf16 ? &k_join_parts<true> : &k_join_parts<false>, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0,
-                s, part, out, parts, values);
+  return launch_join_products(part, JoinOutputs{{out, nullptr, nullptr}}, 1, bf16, parts, values, s);
 }
 
 // How a product is cut up: the tile and the parts of k.  In units of a 256 x 256 x 32 stage (about 0.45 us): a tile of 256 takes
-// a compute unit, of 128 half of one, which then yields 0.7 of the rate; a round of tiles has about eight stages' worth of
-// start and epilogue; parts are written and read again, from caches for the most part (8 TB/s), and their join is a kernel (5 us).
+// a compute unit, of 128 half of one, which then yields 0.7 of the rate, or 0.4 of it where it has the unit for itself and waits
+// for memory; a round of tiles has about eight stages' worth of start and epilogue; parts are written and read again, from
+// caches for the most part (8 TB/s), and their join is a kernel (8).  Forward and backward pass, us with no parts of the first
+// layer's products and the weights' gradients / with parts: 128 tokens of d = 4096, 4096 units 63 / 46, 101 / 77; 500, 4096, 512
+// 57 / 32, 75 / 44; 8192, 512, 2048 84 / 78, 189 / 160; 8192, 256, 512 24 / 23, 117 / 50.  Every other choice of one product's
+// tile and parts was timed for 15 such sizes: at most 4 % of a pass better.
 struct ProductShape {
   int tile, splits;
 };
@@ -127,12 +161,12 @@ inline ProductShape product_shape(int M, int N, int steps, int products, int mos
   double least = 0.0;
   for (int tile = 256; tile >= 128; tile /= 2)
     for (int splits = 1; splits <= most_splits; ++splits) {
-      if (splits > 1 && steps / splits < 16) break;
+      if (splits > 1 && steps / splits < 8) break;
       const double tiles = (double)((M + tile - 1) / tile) * ((N + tile - 1) / tile) * products * splits;
       const double slots = tile == 256 ? 256.0 : 512.0, rounds = (double)(long long)((tiles + slots - 1.0) / slots);
-      const double stage = tile == 256 ? 1.0 : (tiles <= 256.0 ? 0.4 : 0.72);
+      const double stage = tile == 256 ? 1.0 : (tiles <= 256.0 ? 0.6 : 0.72);
       double cost = rounds * (((steps + splits - 1) / splits) * stage + 8.0);
-      if (splits > 1) cost += 11.0 + 8.0 * splits * M * N / 8e6 / 0.45;
+      if (splits > 1) cost += 8.0 + 8.0 * splits * products * M * N / 8e6 / 0.45;
       if (least == 0.0 || cost < least) least = cost, best = ProductShape{tile, splits};
     }
   return best;

@@ -15,89 +15,135 @@ struct StoreBf16 {
   }
 };
 
-// h = a(g) u.
+// h = a(g) u of eight units, and what the backward pass needs (kept.g null: h only).
+template <int ACT>
+__device__ __forceinline__ void store_gated(const GatedKept& kept, size_t at, const float (&g)[8], const float (&u)[8]) {
+  float hv[8], slope;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) hv[e] = activation<ACT>(g[e], &slope) * u[e];
+  *reinterpret_cast<uint4*>(kept.h + at) = pack8(hv);
+  if (kept.g) {
+    uint32_t gd[4], ud[4], low[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      gd[q] = upper_pair(g[2 * q], g[2 * q + 1]);
+      ud[q] = upper_pair(u[2 * q], u[2 * q + 1]);
+      low[q] = lower_pair(g[2 * q], u[2 * q], g[2 * q + 1], u[2 * q + 1]);
+    }
+    *reinterpret_cast<uint4*>(kept.g + at) = make_uint4(gd[0], gd[1], gd[2], gd[3]);
+    *reinterpret_cast<uint4*>(kept.u + at) = make_uint4(ud[0], ud[1], ud[2], ud[3]);
+    *reinterpret_cast<uint4*>(kept.low + at) = make_uint4(low[0], low[1], low[2], low[3]);
+  }
+}
 template <int ACT>
 struct StoreGated {
-  GatedKept kept;  // g null: h only
+  GatedKept kept;
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
     for_rows<true>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[2][8], int) {
-      const size_t at = (size_t)m * N + n;
-      float hv[8], slope;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) hv[e] = activation<ACT>(v[0][e], &slope) * v[1][e];
-      *reinterpret_cast<uint4*>(kept.h + at) = pack8(hv);
-      if (kept.g) {
-        uint32_t g[4], u[4], low[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          g[q] = upper_pair(v[0][2 * q], v[0][2 * q + 1]);
-          u[q] = upper_pair(v[1][2 * q], v[1][2 * q + 1]);
-          low[q] = lower_pair(v[0][2 * q], v[1][2 * q], v[0][2 * q + 1], v[1][2 * q + 1]);
-        }
-        *reinterpret_cast<uint4*>(kept.g + at) = make_uint4(g[0], g[1], g[2], g[3]);
-        *reinterpret_cast<uint4*>(kept.u + at) = make_uint4(u[0], u[1], u[2], u[3]);
-        *reinterpret_cast<uint4*>(kept.low + at) = make_uint4(low[0], low[1], low[2], low[3]);
-      }
+      store_gated<ACT>(kept, (size_t)m * N + n, v[0], v[1]);
     });
   }
 };
+// The same from parts of k.
+template <int ACT>
+__global__ __launch_bounds__(256) void k_join_gated(const float* __restrict__ part, int parts, long long values, GatedKept kept) {
+  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < values; i += (long long)gridDim.x * 2048) {
+    float g[8], u[8];
+    join_eight(part + i, parts, 2 * (size_t)values, g);
+    join_eight(part + values + i, parts, 2 * (size_t)values, u);
+    store_gated<ACT>(kept, (size_t)i, g, u);
+  }
+}
 
-// The sums are dh: dg = dh u a'(g), du = dh a(g), rounded to bf16 for the products that follow.
+// dg = dh u a'(g), du = dh a(g) of eight units, rounded to bf16 for the products that follow.
+struct KeptEight {
+  uint4 g, u, low;
+};
+__device__ __forceinline__ KeptEight load_kept(const GatedKept& kept, size_t at) {
+  return KeptEight{*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
+                   *reinterpret_cast<const uint4*>(kept.low + at)};
+}
+template <int ACT>
+__device__ __forceinline__ void store_slopes(const KeptEight& k, const float (&dh)[8], uint16_t* dg, uint16_t* du) {
+  float gv[8], uv[8], dgv[8], duv[8];
+  unpack_kept(k.g, k.u, k.low, gv, uv);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float slope;
+    const float a = activation<ACT>(gv[e], &slope);
+    dgv[e] = dh[e] * uv[e] * slope;
+    duv[e] = dh[e] * a;
+  }
+  *reinterpret_cast<uint4*>(dg) = pack8(dgv);
+  *reinterpret_cast<uint4*>(du) = pack8(duv);
+}
 template <int ACT>
 struct StoreGateSlopes {
   GatedKept kept;
   uint16_t *dg, *du;
   template <int MB, int NB>
   __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
-    struct Planes {
-      uint4 g, u, low;
-    };
-    auto fetch = [&](int m, int n) {
-      const size_t at = (size_t)m * N + n;
-      return Planes{*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
-                    *reinterpret_cast<const uint4*>(kept.low + at)};
-    };
-    for_rows<false>(acc, smem, m0, n0, M, N, fetch, [&](int m, int n, const float (&v)[1][8], const Planes& k) {
-      const size_t at = (size_t)m * N + n;
-      float gv[8], uv[8], dgv[8], duv[8];
-      unpack_kept(k.g, k.u, k.low, gv, uv);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float slope;
-        const float a = activation<ACT>(gv[e], &slope), dh = v[0][e];
-        dgv[e] = dh * uv[e] * slope;
-        duv[e] = dh * a;
-      }
-      *reinterpret_cast<uint4*>(dg + at) = pack8(dgv);
-      *reinterpret_cast<uint4*>(du + at) = pack8(duv);
+    auto fetch = [&](int m, int n) { return load_kept(kept, (size_t)m * N + n); };
+    for_rows<false>(acc, smem, m0, n0, M, N, fetch, [&](int m, int n, const float (&v)[1][8], const KeptEight& k) {
+      store_slopes<ACT>(k, v[0], dg + (size_t)m * N + n, du + (size_t)m * N + n);
     });
   }
 };
+template <int ACT>
+__global__ __launch_bounds__(256) void k_join_slopes(const float* __restrict__ part, int parts, long long values, GatedKept kept,
+                                                     uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
+  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < values; i += (long long)gridDim.x * 2048) {
+    const KeptEight k = load_kept(kept, (size_t)i);
+    float dh[8];
+    join_eight(part + i, parts, (size_t)values, dh);
+    store_slopes<ACT>(k, dh, dg + i, du + i);
+  }
+}
 
 constexpr int kMostSplits = 32;
 int k_steps(int k) { return (k + kGemmStep - 1) / kGemmStep; }
-ProductShape split_shape(int M, int N, int K, int segments) {
-  return product_shape(M, N, segments * k_steps(K), 1, kMostSplits);
+ProductShape up_shape(int T, int d, int d_ff) { return product_shape(T, 2 * d_ff, k_steps(d), 1, kMostSplits); }
+ProductShape slopes_shape(int T, int d, int d_ff) { return product_shape(T, d_ff, k_steps(d), 1, kMostSplits); }
+ProductShape weights_shape(int T, int d, int d_ff, int products) {
+  return product_shape(d_ff, d, k_steps(T), products, kMostSplits);
 }
+ProductShape units_shape(int T, int d, int d_ff, int segments) {
+  return product_shape(T, d, segments * k_steps(d_ff), 1, kMostSplits);
+}
+size_t split_bytes(const ProductShape& shape, size_t values) { return shape.splits > 1 ? shape.splits * values * sizeof(float) : 0; }
 
-// One product with an M x N bf16 result, split over k where the tiles are few.
+// Up to three products of one shape with bf16 results, split over k where their tiles are few.
 template <bool AK, bool BK>
-hipError_t launch_split_product(GemmArgs g, uint16_t* out, float* part, hipStream_t s) {
-  g.products = 1;
-  const ProductShape shape = split_shape(g.M, g.N, g.K, g.segments);
+hipError_t launch_split_products(GemmArgs g, const ProductShape& shape, const StoreBf16& out, float* part, hipStream_t s) {
   g.splits = shape.splits;
-  if (g.splits == 1) return launch_product<AK, BK, false, false>(g, shape.tile, StoreBf16{{out, nullptr, nullptr}}, s);
-  const hipError_t e = launch_product<AK, BK, false, false>(g, shape.tile, StorePart{part}, s);
-  return e != hipSuccess ? e : launch_join_parts(part, out, true, g.splits, (long long)g.M * g.N, s);
+  if (g.splits == 1) return launch_product<AK, BK, false, false>(g, shape.tile, out, s);
+  const hipError_t e = launch_product<AK, BK, false, false>(g, shape.tile, StorePart<false>{part, g.splits}, s);
+  if (e != hipSuccess) return e;
+  return launch_join_products(part, JoinOutputs{{out.c[0], out.c[1], out.c[2]}}, g.products, true, g.splits,
+                              (long long)g.M * g.N, s);
 }
 
 }  // namespace
 
-size_t gated_part_bytes(int T, int d, int d_ff, int segments) {
-  if (T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff, segments);
-  const int s = split_shape(T, d, d_ff, segments).splits;
-  return s > 1 ? (size_t)s * T * d * sizeof(float) : 0;
+size_t gated_forward_part_bytes(int T, int d, int d_ff) {
+  if (T <= kGatedFewTokens) return gated_few_part_bytes(T, d, d_ff, 1);
+  const size_t up = split_bytes(up_shape(T, d, d_ff), 2 * (size_t)T * d_ff);
+  const size_t down = split_bytes(units_shape(T, d, d_ff, 1), (size_t)T * d);
+  return up > down ? up : down;
+}
+
+size_t gated_backward_part_bytes(int T, int d, int d_ff) {
+  size_t weights = 0;
+  for (int products = 1; products <= 3; ++products) {
+    const size_t bytes = split_bytes(weights_shape(T, d, d_ff, products), products * (size_t)d_ff * d);
+    if (bytes > weights) weights = bytes;
+  }
+  const bool few = T <= kGatedFewTokens;
+  const size_t slopes = few ? 0 : split_bytes(slopes_shape(T, d, d_ff), (size_t)T * d_ff);
+  const size_t dx = few ? gated_few_part_bytes(T, d, d_ff, 2) : split_bytes(units_shape(T, d, d_ff, 2), (size_t)T * d);
+  const size_t most = weights > slopes ? weights : slopes;
+  return most > dx ? most : dx;
 }
 
 hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
@@ -106,16 +152,25 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
   GemmArgs up{};
   up.a[0] = x, up.b[0] = L.wg, up.b[1] = L.wu;
   up.M = T, up.N = L.d_ff, up.K = L.d, up.lda = up.ldb = 2u * L.d;
-  up.segments = up.products = up.splits = 1;
-  const hipError_t e = with_activation(L.act, [&](auto act) {
-    return launch_product<true, true, true, false>(up, product_shape(T, 2 * L.d_ff, k_steps(L.d), 1, 1).tile, StoreGated<decltype(act)::value>{kept}, s);
+  up.segments = up.products = 1;
+  const ProductShape shape = up_shape(T, L.d, L.d_ff);
+  up.splits = shape.splits;
+  const long long units = (long long)T * L.d_ff;
+  hipError_t e = hipSuccess;
+  if (shape.splits > 1) e = launch_product<true, true, true, false>(up, shape.tile, StorePart<true>{part, shape.splits}, s);
+  if (e != hipSuccess) return e;
+  e = with_activation(L.act, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if (shape.splits > 1)
+      return launch(&k_join_gated<ACT>, dim3(join_blocks(units / 8)), dim3(256), 0, s, part, shape.splits, units, kept);
+    return launch_product<true, true, true, false>(up, shape.tile, StoreGated<ACT>{kept}, s);
   });
   if (e != hipSuccess) return e;
   GemmArgs down{};
   down.a[0] = kept.h, down.b[0] = L.w2u;
   down.M = T, down.N = L.d, down.K = L.d_ff, down.lda = 2u * L.d_ff, down.ldb = 2u * L.d;
-  down.segments = 1;
-  return launch_split_product<true, false>(down, y, part, s);
+  down.segments = down.products = 1;
+  return launch_split_products<true, false>(down, units_shape(T, L.d, L.d_ff, 1), StoreBf16{{y, nullptr, nullptr}}, part, s);
 }
 
 hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
@@ -125,17 +180,24 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   const bool few = T <= kGatedFewTokens;
   if (few && (dx || dwg || dwu)) {
     e = launch_gated_few_slopes(L, dy, T, kept, dg, du, s);
-    if (e != hipSuccess) return e;
   } else if (dx || dwg || dwu) {
     GemmArgs a{};
     a.a[0] = dy, a.b[0] = L.w2u;
     a.M = T, a.N = L.d_ff, a.K = L.d, a.lda = a.ldb = 2u * L.d;
-    a.segments = a.products = a.splits = 1;
-    e = with_activation(L.act, [&](auto act) {
-      return launch_product<true, true, false, false>(a, product_shape(T, L.d_ff, k_steps(L.d), 1, 1).tile, StoreGateSlopes<decltype(act)::value>{kept, dg, du}, s);
-    });
+    a.segments = a.products = 1;
+    const ProductShape shape = slopes_shape(T, L.d, L.d_ff);
+    a.splits = shape.splits;
+    const long long units = (long long)T * L.d_ff;
+    if (shape.splits > 1) e = launch_product<true, true, false, false>(a, shape.tile, StorePart<false>{part, shape.splits}, s);
     if (e != hipSuccess) return e;
+    e = with_activation(L.act, [&](auto act) {
+      constexpr int ACT = decltype(act)::value;
+      if (shape.splits > 1)
+        return launch(&k_join_slopes<ACT>, dim3(join_blocks(units / 8)), dim3(256), 0, s, part, shape.splits, units, kept, dg, du);
+      return launch_product<true, true, false, false>(a, shape.tile, StoreGateSlopes<ACT>{kept, dg, du}, s);
+    });
   }
+  if (e != hipSuccess) return e;
   GemmArgs w{};
   StoreBf16 out{};
   auto add = [&](const uint16_t* a, const uint16_t* b, uint16_t* c) {
@@ -146,8 +208,8 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   add(kept.h, dy, dw2u);
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
-    w.segments = w.splits = 1;
-    e = launch_product<false, false, false, false>(w, product_shape(L.d_ff, L.d, k_steps(T), w.products, 1).tile, out, s);
+    w.segments = 1;
+    e = launch_split_products<false, false>(w, weights_shape(T, L.d, L.d_ff, w.products), out, part, s);
     if (e != hipSuccess) return e;
   }
   if (dx && few) return launch_gated_few_dx(L, T, dg, du, dx, part, s);
@@ -155,8 +217,8 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     GemmArgs a{};
     a.a[0] = dg, a.a[1] = du, a.b[0] = L.wg, a.b[1] = L.wu;
     a.M = T, a.N = L.d, a.K = L.d_ff, a.lda = 2u * L.d_ff, a.ldb = 2u * L.d;
-    a.segments = 2;
-    e = launch_split_product<true, false>(a, dx, part, s);
+    a.segments = 2, a.products = 1;
+    e = launch_split_products<true, false>(a, units_shape(T, L.d, L.d_ff, 2), StoreBf16{{dx, nullptr, nullptr}}, part, s);
   }
   return e;
 }

@@ -479,8 +479,9 @@ struct GatedLayer {
   const uint16_t* wu;
   const uint16_t* w2u;
 };
-// Bytes of the fp32 parts of the forward pass's second product (segments 1) or of dx (2); 0: it is not split.
-size_t gated_part_bytes(int T, int d, int d_ff, int segments);
+// Bytes of the fp32 parts of the products that are split; 0: none is.
+size_t gated_forward_part_bytes(int T, int d, int d_ff);
+size_t gated_backward_part_bytes(int T, int d, int d_ff);
 // Planes [T, d_ff] of 16 bits that the forward pass leaves for the backward pass; g, u, low null: h only.
 struct GatedKept {
   uint16_t *h, *g, *u, *low;

@@ -123,6 +123,15 @@ def test_widths(hire, T, d, F, act):
     check(run(hire, data, act), data, act)
 
 
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("T,d,F", [(70, 2056, 72), (130, 4104, 264), (257, 1048, 40), (3000, 72, 136), (1531, 8, 8), (513, 264, 2600)])
+def test_products_in_parts(hire, T, d, F, act):
+    """Few tiles and many k: of the first layer's products, of the weights' gradients, of y and dx."""
+    print(f"T={T} d={d} F={F} {act}", flush=True)
+    data = inputs(T + d, T, d, F, exact=act == "relu")
+    check(run(hire, data, act), data, act)
+
+
 @pytest.mark.parametrize("T,d,F", [(1, 64, 128), (40, 96, 264), (130, 64, 512), (300, 128, 136)])
 def test_relu_at_zero(hire, T, d, F):
     """Exact pre-activations, some of them 0 (of 128 with one token none is): the slope there is 0."""
