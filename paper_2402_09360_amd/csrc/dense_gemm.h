@@ -199,8 +199,10 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int m0 = (8 * group + in % gm) * TILE, n0 = in / gm * n_tile;
 
   const int seg_steps = (g.K + kGemmStep - 1) / kGemmStep, steps = seg_steps * g.segments;
-  const int s0 = (int)((long long)steps * split / g.splits);
-  const int n = (int)((long long)steps * (split + 1) / g.splits) - s0;
+  constexpr int kTurn = MX ? 4 : 1;  // stages that share a load of scale bytes stay together
+  const int turns = (steps + kTurn - 1) / kTurn;
+  const int s0 = kTurn * (int)((long long)turns * split / g.splits);
+  const int n = min(steps, kTurn * (int)((long long)turns * (split + 1) / g.splits)) - s0;
 
   TA ta;
   TB tb;
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(2 * TILE) __attribute__((amdgpu_waves_per_eu(2, 2))
   if constexpr (MX) {
     const bool of_a = wave < kWaves / 2;
     const int row0 = of_a ? m0 : n0, last = (of_a ? g.M : g.N) - 1 - row0;
-    scales = reinterpret_cast<const char*>(of_a ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld;
+    scales = reinterpret_cast<const char*>(of_a ? g.a_scales : g.b_scales) + (size_t)row0 * g.scale_ld + 4 * s0;
     scale_off = (uint32_t)min(wave % (kWaves / 2) * 64 + lane_id(), last) * g.scale_ld;
   }
   // the next stage to request: its place, addresses and what is left of its segment of k

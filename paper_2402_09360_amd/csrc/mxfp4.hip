@@ -463,14 +463,14 @@ __global__ __launch_bounds__(64 * RW * KW) void k_mx_shared(const uint8_t* __res
 }
 
 // ---- packed tokens in tiles ----------------------------------------------------------
-// y's rows out of the sums: whole vectors where the row length admits them.
+// y's rows out of the sums: whole vectors where the row length admits them.  Parts of the columns follow one another, in fp32.
 struct StoreProduct {
   void* y;
   int bf16;
   template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int) const {
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int, int split) const {
     for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
-      const size_t at = (size_t)m * N + n;
+      const size_t at = ((size_t)split * M + m) * N + n;
       if (N % 8 != 0) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -610,9 +610,6 @@ namespace {
 bool mx_pads_scales(const MxProduct& p) {
   return p.cols % 512 != 0 || reinterpret_cast<uintptr_t>(p.x_scales) % 16 != 0 || reinterpret_cast<uintptr_t>(p.scales) % 16 != 0;
 }
-}  // namespace
-
-namespace {
 // Packed tokens as tiles of a dense product: always from 65 on, and where the rows are many enough for tiles of 128 of them; a few
 // tokens' tiles are mostly empty, but the tokens then come to LDS once for 128 rows.  us with the few tokens' kernel / as tiles,
 // 2048 columns: 256000 rows, 17 tokens 77 / 71, 64 128 / 79; 16384, 17 8.7 / 9.7, 33 10.2 / 9.9, 64 13.0 / 10.5; 1000 of 8192, 64
@@ -620,16 +617,23 @@ namespace {
 bool mx_tiles(int T, int rows) {
   return T > kMxFewTokens || (T > 32 && rows >= 16384) || (T > 8 && rows >= 65536);
 }
-size_t mx_padded_bytes(int T, int rows, int cols) { return ((size_t)T + rows) * ((cols / kMxBlock + 15) / 16) * 16; }
+size_t mx_padded_bytes(int T, int rows, int cols) {
+  return (((size_t)T + rows) * ((cols / kMxBlock + 15) / 16) * 16 + 255) / 256 * 256;
+}
+// Tiles that leave compute units idle in parts of the columns, whose sums are joined.  us without / with: 100 tokens on 1000 rows
+// of 8192 columns 28.2 / 12.7, on 8192 rows 30.5 / 19.9; 1000 on 1024 of 8192 28.2 / 23.3; 128 on 2048 of 4096 16.5 / 11.7.  Every
+// other tile and number of parts was timed for 16 such sizes: at most 9 % better.
+ProductShape mx_shape(int T, int rows, int cols) { return product_shape(T, rows, (cols + 127) / 128, 1, 32); }
+size_t mx_parts_bytes(int splits, int T, int rows) { return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0; }
 }  // namespace
 
-// Room for the parts of few tokens' sums and for the padded scale bytes of tiles, whichever the call needs.
+// Room for the parts of the sums and, with tiles, for padded scale bytes in front of them, whichever the call needs.
 size_t mx_workspace_bytes(int T, int rows, int cols) {
-  const size_t padded = mx_tiles(T, rows) ? mx_padded_bytes(T, rows, cols) : 0;
-  if (T > kMxFewTokens) return padded;
-  const int splits = few_splits(T, rows, cols);
-  const size_t parts = splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0;
-  return parts > padded ? parts : padded;
+  const size_t tiles =
+      mx_tiles(T, rows) ? mx_padded_bytes(T, rows, cols) + mx_parts_bytes(mx_shape(T, rows, cols).splits, T, rows) : 0;
+  if (T > kMxFewTokens) return tiles;
+  const size_t parts = mx_parts_bytes(few_splits(T, rows, cols), T, rows);
+  return parts > tiles ? parts : tiles;
 }
 
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
@@ -639,7 +643,8 @@ hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
   GemmArgs g{};
   g.a[0] = p.x, g.b[0] = p.codes;
   g.M = p.T, g.N = p.rows, g.K = p.cols / 4, g.lda = g.ldb = (uint32_t)p.cols / 2;
-  g.segments = g.products = g.splits = 1;
+  const ProductShape shape = mx_shape(p.T, p.rows, p.cols);
+  g.segments = g.products = 1, g.splits = shape.splits;
   g.a_scales = p.x_scales, g.b_scales = p.scales, g.scale_ld = 4u * words;
   if (mx_pads_scales(p)) {
     uint32_t* padded = static_cast<uint32_t*>(p.workspace);
@@ -654,8 +659,10 @@ hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
     g.a_scales = reinterpret_cast<const uint8_t*>(padded);
     g.b_scales = reinterpret_cast<const uint8_t*>(padded + (size_t)p.T * words);
   }
-  const int tile = product_shape(p.T, p.rows, (p.cols + 127) / 128, 1, 1).tile;
-  return launch_product<true, true, false, true>(g, tile, StoreProduct{p.y, p.y_bf16}, s);
+  if (g.splits == 1) return launch_product<true, true, false, true>(g, shape.tile, StoreProduct{p.y, p.y_bf16}, s);
+  float* part = reinterpret_cast<float*>(static_cast<char*>(p.workspace) + mx_padded_bytes(p.T, p.rows, p.cols));
+  const hipError_t e = launch_product<true, true, false, true>(g, shape.tile, StoreProduct{part, 0}, s);
+  return e != hipSuccess ? e : launch_join_parts(part, p.y, p.y_bf16 != 0, g.splits, (long long)p.T * p.rows, s);
 }
 
 }  // namespace hire

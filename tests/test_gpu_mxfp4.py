@@ -174,6 +174,14 @@ def test_many_tokens(hire, T, rows, cols, dtype):
     product_case(hire, T, rows, cols, True, dtype)
 
 
+@pytest.mark.parametrize("T,rows,cols", [(65, 1, 4128), (100, 257, 8224), (300, 40, 16384), (1021, 77, 8192), (130, 512, 2048)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_products_in_parts(hire, T, rows, cols, dtype):
+    """Few tiles of long rows."""
+    print(f"T={T} {rows}x{cols}", flush=True)
+    product_case(hire, T, rows, cols, True, dtype)
+
+
 @pytest.mark.parametrize("rows,cols", [(40000, 256), (33000, 96), (3, 65536)])
 def test_long_matrices(hire, rows, cols):
     for T, packed in ((1, False), (1, True), (20, False), (64, False), (50, True)):
