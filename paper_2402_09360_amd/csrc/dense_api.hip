@@ -66,6 +66,16 @@ int check_drafts(const hire_drafts* D) {
   return HIRE_OK;
 }
 
+DraftArgs draft_args(const hire_drafts* D) {
+  DraftArgs a{};
+  a.B = D->B, a.n = D->n, a.vocab = D->vocab;
+  a.lengths = D->lengths, a.tokens = D->tokens;
+  a.target = D->target_prob, a.target_idx = D->target_idx, a.target_k = D->target_k;
+  a.draft = D->draft_prob, a.draft_idx = D->draft_idx, a.draft_k = D->draft_k;
+  a.accept_u = D->accept_u, a.sample_u = D->sample_u;
+  return a;
+}
+
 size_t hidden_bytes(const hire_gated_layer* L, int T) { return align_up((size_t)T * L->d_ff * 2); }
 GatedKept kept_planes(const hire_gated_layer* L, int T, void* saved) {
   const size_t plane = hidden_bytes(L, T);
@@ -151,8 +161,7 @@ int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const voi
 
 size_t hire_verify_draft_workspace_bytes(const hire_drafts* D) {
   if (check_drafts(D) != HIRE_OK) return 0;
-  if (D->target_idx) return kAlign;
-  return align_up(draft_part_bytes(D->B, D->vocab));
+  return D->target_idx ? kAlign : align_up(draft_part_bytes(draft_args(D)));
 }
 
 int hire_verify_draft(const hire_drafts* D, int32_t* tokens_out, int32_t* accepted_out, void* workspace,
@@ -160,12 +169,7 @@ int hire_verify_draft(const hire_drafts* D, int32_t* tokens_out, int32_t* accept
   if (const int rc = check_drafts(D); rc != HIRE_OK) return rc;
   if (!given(tokens_out, 4) || !given(accepted_out, 4) || !given(workspace, 256)) return HIRE_EINVAL;
   if (workspace_bytes < hire_verify_draft_workspace_bytes(D)) return HIRE_ENOSPC;
-  DraftArgs a{};
-  a.B = D->B, a.n = D->n, a.vocab = D->vocab;
-  a.lengths = D->lengths, a.tokens = D->tokens;
-  a.target = D->target_prob, a.target_idx = D->target_idx, a.target_k = D->target_k;
-  a.draft = D->draft_prob, a.draft_idx = D->draft_idx, a.draft_k = D->draft_k;
-  a.accept_u = D->accept_u, a.sample_u = D->sample_u;
+  DraftArgs a = draft_args(D);
   a.out_tokens = tokens_out, a.accepted = accepted_out;
   a.part = static_cast<double*>(workspace);
   return launched(launch_verify(a, static_cast<hipStream_t>(stream)));

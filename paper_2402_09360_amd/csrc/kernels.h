@@ -545,8 +545,7 @@ struct DraftArgs {
 struct DraftParts {
   int count, size;
 };
-DraftParts draft_parts(int B, int vocab);  // dense target
-size_t draft_part_bytes(int B, int vocab);
+size_t draft_part_bytes(const DraftArgs& a);  // dense target
 hipError_t launch_verify(DraftArgs a, hipStream_t s);
 
 // The HIP error behind the calling thread's most recent HIRE_ELAUNCH (api.hip).

@@ -508,11 +508,13 @@ __global__ __launch_bounds__(256) void k_pad_scales(const uint8_t* __restrict__ 
 bool whole_words(const MxProduct& p) { return p.cols % 128 == 0 && reinterpret_cast<uintptr_t>(p.scales) % 4 == 0; }
 
 // How the rows are divided: `groups` sixteens of them for a workgroup, whose waves take the columns in turns of `turn` steps.  More
-// rows share what is read of the tokens (16 kB per step of 64 tokens, against 1 kB of sixteen rows), but 256 workgroups should
-// be left; beyond sixteen tokens the columns are split where they are fewer, and the parts joined.  us with 4 groups, 8 waves / 2, 8 /
-// 1, 16 (and 4, 4 in turns of four): 64 tokens, 1000 rows of 4096 14.4 / 11.3 / 12.9, 2500 15.4 / 13.3 / 19.0, 5000 18.2 / 22.0 / 36.6, of 1024 11.9 / 8.7 /
-// 12.8, 9000 of 4096 28.0 / 42.5 / 54.2, 16384 29.8 / 43.6 / 73.3 (29.0),
-// of 2048 18.6 / - / - (17.1); 20 tokens, 9000 of 1024 7.0 / 7.4 / 9.3, 2500 6.7 / 6.1 / 6.1.
+// rows share what is read of the tokens (16 kB per step of 64 tokens, against 1 kB of sixteen rows), but 256 workgroups should be
+// left; where they are fewer the columns are split and the parts joined.  us with 4 groups, 8 waves / 2, 8 / 1, 16 (and 4, 4 in
+// turns of four): 64 tokens, 1000 rows of 4096 14.4 / 11.3 / 12.9, 2500 15.4 / 13.3 / 19.0, 5000 18.2 / 22.0 / 36.6, of 1024 11.9
+// / 8.7 / 12.8, 9000 of 4096 28.0 / 42.5 / 54.2, 16384 29.8 / 43.6 / 73.3 (29.0), of 2048 18.6 / - / - (17.1); 20 tokens, 9000 of
+// 1024 7.0 / 7.4 / 9.3, 2500 6.7 / 6.1 / 6.1.
+//   Up to sixteen tokens a wave has to have three turns for the join to pay: 100 rows, two tokens / sixteen, us without / with
+// parts: of 8192 columns 8.0 / 12.8, 5.9 / 7.5, of 32768 25.2 / 44.0, 8.6 / 11.0; 1000 rows of 4096 (two turns) 5.7 / 8.1, 6.1 / 7.4.
 struct FewShape {
   int groups, waves, turn;
 };
@@ -526,7 +528,8 @@ int few_splits(int T, int rows, int cols) {
   const FewShape f = few_shape(T, rows);
   const int workgroups = (rows + 16 * f.groups - 1) / (16 * f.groups), turns = (cols + 128 * f.turn - 1) / (128 * f.turn);
   const int fill = 256 / workgroups, most = turns / f.waves;  // a turn for every wave
-  const int splits = T <= 16 ? 1 : (fill < most ? fill : most);
+  if (T <= 16 && most < 3) return 1;
+  const int splits = fill < most ? fill : most;
   return splits < 1 ? 1 : splits;
 }
 

@@ -16,20 +16,28 @@ constexpr int kVerifyThreads = 256;  // one workgroup for a sequence; or that su
 constexpr int kVerifyWaves = kVerifyThreads / kWave;
 constexpr int kPartSlices = kVerifyWaves;  // of a part, one per wave
 
-// Probability of a token by the first entry of a list that names it; whole wave, every lane gets it.
-__device__ __forceinline__ float list_at(const float* prob, const int32_t* idx, int k, int token) {
-  constexpr int kAhead = 8;  // loads under way
-  for (int j0 = 0; j0 < k; j0 += kWave * kAhead) {
-    int32_t name[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) name[u] = idx[min(j0 + u * kWave + lane_id(), k - 1)];
+// Places of the first entries of two lists that name a token, -1: none (k = 0: no list); whole wave, every lane gets them.
+__device__ __forceinline__ void find_in_lists(const int32_t* a, int ka, const int32_t* b, int kb, int token, int* at_a, int* at_b) {
+  constexpr int kAhead = 8;  // loads of each list under way
+  *at_a = *at_b = -1;
+  for (int j0 = 0; j0 < ka || j0 < kb; j0 += kWave * kAhead) {
+    int32_t of_a[kAhead], of_b[kAhead];
+    const bool more_a = j0 < ka && *at_a < 0, more_b = j0 < kb && *at_b < 0;  // uniform
+    if (!more_a && !more_b) return;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const uint64_t hit = __ballot(j0 + u * kWave + lane_id() < k && name[u] == token);
-      if (hit != 0ull) return prob[j0 + u * kWave + __builtin_ctzll(hit)];
+      const int j = j0 + u * kWave + lane_id();
+      if (more_a) of_a[u] = a[min(j, ka - 1)];
+      if (more_b) of_b[u] = b[min(j, kb - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = j0 + u * kWave + lane_id();
+      const uint64_t hit_a = __ballot(more_a && j < ka && of_a[u] == token), hit_b = __ballot(more_b && j < kb && of_b[u] == token);
+      if (*at_a < 0 && hit_a != 0ull) *at_a = j0 + u * kWave + (int)__builtin_ctzll(hit_a);
+      if (*at_b < 0 && hit_b != 0ull) *at_b = j0 + u * kWave + (int)__builtin_ctzll(hit_b);
     }
   }
-  return 0.0f;
 }
 
 __device__ __forceinline__ const float* target_row(const DraftArgs& a, int b, int i) {
@@ -50,27 +58,28 @@ __device__ __forceinline__ int draft_length(const DraftArgs& a, int b) {
 
 // Number of accepted tokens of sequence b, for the whole workgroup; ok: LDS, kMaxDraft words.
 __device__ __forceinline__ int accepted_tokens(const DraftArgs& a, int b, int length, int* ok) {
-  auto decide = [&](int i, auto p_of, auto q_of) {
-    const int d = a.tokens[(size_t)b * a.n + i];
-    if ((unsigned)d >= (unsigned)a.vocab) return 0;
-    const double p = p_of(i, d), q = q_of(i, d);
-    return (double)a.accept_u[(size_t)b * a.n + i] * q < p ? 1 : 0;
-  };
+  auto drafted = [&](int i) { return a.tokens[(size_t)b * a.n + i]; };
+  auto decide = [&](int i, float p, float q) { return (double)a.accept_u[(size_t)b * a.n + i] * (double)q < (double)p ? 1 : 0; };
   if (!a.target_idx && !a.draft_idx) {  // a lane for each token
-    if (threadIdx.x < kMaxDraft && (int)threadIdx.x < length)
-      ok[threadIdx.x] = decide((int)threadIdx.x, [&](int i, int d) { return target_row(a, b, i)[d]; },
-                               [&](int i, int d) { return a.draft ? draft_row(a, b, i)[d] : 1.0f; });
+    const int i = (int)threadIdx.x;
+    if (i < kMaxDraft && i < length) {
+      const int d = drafted(i);
+      ok[i] = (unsigned)d < (unsigned)a.vocab ? decide(i, target_row(a, b, i)[d], a.draft ? draft_row(a, b, i)[d] : 1.0f) : 0;
+    }
   } else {  // a wave for each
     for (int i = wave_id(); i < length; i += (int)(blockDim.x / kWave)) {
-      const int yes = decide(
-          i,
-          [&](int t, int d) {
-            return a.target_idx ? list_at(target_row(a, b, t), target_list(a, b, t), a.target_k, d) : target_row(a, b, t)[d];
-          },
-          [&](int t, int d) {
-            return a.draft_idx ? list_at(draft_row(a, b, t), draft_list(a, b, t), a.draft_k, d)
-                               : (a.draft ? draft_row(a, b, t)[d] : 1.0f);
-          });
+      const int d = drafted(i);
+      int yes = 0;
+      if ((unsigned)d < (unsigned)a.vocab) {
+        int in_p, in_q;
+        find_in_lists(a.target_idx ? target_list(a, b, i) : nullptr, a.target_idx ? a.target_k : 0,
+                      a.draft_idx ? draft_list(a, b, i) : nullptr, a.draft_idx ? a.draft_k : 0, d, &in_p, &in_q);
+        if (!a.target_idx) in_p = d;
+        if (!a.draft_idx) in_q = d;
+        const float p = in_p >= 0 ? target_row(a, b, i)[in_p] : 0.0f;
+        const float q = !a.draft ? 1.0f : (in_q >= 0 ? draft_row(a, b, i)[in_q] : 0.0f);
+        yes = decide(i, p, q);
+      }
       if (lane_id() == 0) ok[i] = yes;
     }
   }
@@ -84,14 +93,15 @@ __device__ __forceinline__ int accepted_tokens(const DraftArgs& a, int b, int le
 struct Running {
   double before[2], total[2];
 };
-__device__ __forceinline__ Running running_sums(double x, double y, double (&waves)[2][kVerifyWaves]) {
+template <int WAVES>
+__device__ __forceinline__ Running running_sums(double x, double y, double (&waves)[2][WAVES]) {
   auto add = [](double p, double q) { return p + q; };
   const double ix = wave_prefix(x, 0.0, add), iy = wave_prefix(y, 0.0, add);
   if (lane_id() == kWave - 1) waves[0][wave_id()] = ix, waves[1][wave_id()] = iy;
   __syncthreads();
   Running r{{0.0, 0.0}, {0.0, 0.0}};
 #pragma unroll
-  for (int w = 0; w < kVerifyWaves; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     if (w == wave_id()) r.before[0] = r.total[0], r.before[1] = r.total[1];
     r.total[0] += waves[0][w];
     r.total[1] += waves[1][w];
@@ -108,8 +118,8 @@ struct Found {
   int hit, last;
   double before_hit, before_last;
 };
-template <int EACH>
-__device__ __forceinline__ int find_place(const double (&w)[EACH], double before, double mark, Found (&waves)[kVerifyWaves],
+template <int EACH, int WAVES>
+__device__ __forceinline__ int find_place(const double (&w)[EACH], double before, double mark, Found (&waves)[WAVES],
                                           double* start) {
   Found f{-1, -1, 0.0, 0.0};
   double sum = before;
@@ -128,7 +138,7 @@ __device__ __forceinline__ int find_place(const double (&w)[EACH], double before
   __syncthreads();
   Found r{-1, -1, 0.0, 0.0};
 #pragma unroll
-  for (int v = kVerifyWaves - 1; v >= 0; --v) {
+  for (int v = WAVES - 1; v >= 0; --v) {
     const Found o = waves[v];
     if (o.hit >= 0) r.hit = o.hit, r.before_hit = o.before_hit;
     if (r.last < 0 && o.last >= 0) r.last = o.last, r.before_last = o.before_last;
@@ -144,13 +154,15 @@ __device__ __forceinline__ void write_tokens(const DraftArgs& a, int b, int acce
 }
 
 // ---- target as lists: a workgroup per sequence ------------------------------------
+// Bound by the chain of its steps, not by bytes.  Four drafted tokens, 64 sequences, lists of 1024 of 32000 tokens: 16.9 us (21.3
+// with four waves, four entries in a thread).
 // A table in LDS tells for a token the first place of a list that names it: open addressing, at most half full.
 struct PlaceTable {
   int32_t* key;
   int32_t* place;
   int mask;
   __device__ __forceinline__ void clear() const {
-    for (int i = threadIdx.x; i <= mask; i += kVerifyThreads) key[i] = -1, place[i] = 0x7FFFFFFF;
+    for (int i = threadIdx.x; i <= mask; i += (int)blockDim.x) key[i] = -1, place[i] = 0x7FFFFFFF;
     __syncthreads();
   }
   __device__ __forceinline__ int slot(int token) const { return (int)((uint32_t)token * 2654435761u >> 16) & mask; }
@@ -171,12 +183,12 @@ struct PlaceTable {
   }
 };
 
-template <int EACH>  // places of a thread
-__global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
-  constexpr int kSlots = 2 * EACH * kVerifyThreads;
+template <int THREADS, int EACH>  // places of a thread
+__global__ __launch_bounds__(THREADS) void k_verify_lists(DraftArgs a) {
+  constexpr int kSlots = 2 * EACH * THREADS;
   __shared__ int ok[kMaxDraft];
-  __shared__ double waves[2][kVerifyWaves];
-  __shared__ Found found[kVerifyWaves];
+  __shared__ double waves[2][THREADS / kWave];
+  __shared__ Found found[THREADS / kWave];
   __shared__ int32_t keys[kSlots], places[kSlots];
   const int b = blockIdx.x, length = draft_length(a, b);
   const double sample = (double)a.sample_u[b];
@@ -195,7 +207,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
     const int at = min(first + i, a.target_k - 1);
     token[i] = tokens[at];
     whole[i] = (double)p[at];
-    if (by_list) other[i] = draft_list(a, b, accepted)[min((int)threadIdx.x + i * kVerifyThreads, a.draft_k - 1)];
+    if (by_list) other[i] = draft_list(a, b, accepted)[min((int)threadIdx.x + i * THREADS, a.draft_k - 1)];
   }
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
@@ -211,7 +223,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
     table.clear();
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int j = (int)threadIdx.x + i * kVerifyThreads;
+      const int j = (int)threadIdx.x + i * THREADS;
       if (j < a.draft_k && (unsigned)other[i] < (unsigned)a.vocab) table.insert(other[i], j);
     }
     __syncthreads();
@@ -239,7 +251,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_lists(DraftArgs a) {
 #pragma unroll
   for (int i = 0; i < EACH; ++i) rest[i] = nothing ? whole[i] : rest[i];
   double start;
-  const int at = find_place<EACH>(rest, nothing ? r.before[1] : r.before[0], sample * (nothing ? r.total[1] : r.total[0]), found,
+  const int at = find_place(rest, nothing ? r.before[1] : r.before[0], sample * (nothing ? r.total[1] : r.total[0]), found,
                                   &start);
   write_tokens(a, b, accepted, at >= 0 ? tokens[at] : -1);
 }
@@ -400,7 +412,8 @@ __device__ __forceinline__ PartDraft<KIND> part_draft(const DraftArgs& a, int b,
   }
   d.row = draft_row(a, b, accepted);
   if constexpr (KIND == kDraftList) {
-    for (int i = threadIdx.x; i < size; i += blockDim.x) places[i] = 0x7FFFFFFF;
+    const int4 none = make_int4(0x7FFFFFFF, 0x7FFFFFFF, 0x7FFFFFFF, 0x7FFFFFFF);
+    for (int i = threadIdx.x; i < size / 4; i += blockDim.x) reinterpret_cast<int4*>(places)[i] = none;
     __syncthreads();
     const int32_t* list = draft_list(a, b, accepted);
     for (int j = threadIdx.x; j < a.draft_k; j += blockDim.x) {
@@ -414,10 +427,11 @@ __device__ __forceinline__ PartDraft<KIND> part_draft(const DraftArgs& a, int b,
 
 // A wave sums a quarter of the workgroup's part, so that the one behind has less to look through; the first workgroup of a
 // sequence leaves how many tokens were accepted.  VEC: rows start at multiples of 16 bytes.
-template <int KIND, bool VEC>
+// PART: the most tokens of a part.
+template <int KIND, bool VEC, int PART>
 __global__ __launch_bounds__(kVerifyThreads) void k_verify_sums(DraftArgs a) {
   __shared__ int ok[kMaxDraft];
-  __shared__ int32_t places[KIND == kDraftList ? kMaxDraftPart : 1];
+  __shared__ __align__(16) int32_t places[KIND == kDraftList ? PART : 4];
   const int b = blockIdx.y, length = draft_length(a, b);
   const int accepted = accepted_tokens(a, b, length, ok);
   if (blockIdx.x == 0 && threadIdx.x == 0) a.accepted[b] = accepted;
@@ -450,6 +464,12 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_sums(DraftArgs a) {
           const float qe[4] = {qv[u].x, qv[u].y, qv[u].z, qv[u].w};
 #pragma unroll
           for (int e = 0; e < 4; ++e) add(pe[e], q.refused ? (double)qe[e] : 0.0);
+        } else if constexpr (KIND == kDraftList) {
+          int4 in = make_int4(0x7FFFFFFF, 0x7FFFFFFF, 0x7FFFFFFF, 0x7FFFFFFF);
+          if (q.refused) in = *reinterpret_cast<const int4*>(places + (at - v0));
+          const int j[4] = {in.x, in.y, in.z, in.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) add(pe[e], j[e] != 0x7FFFFFFF ? (double)q.row[j[e]] : 0.0);
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) add(pe[e], q.at(at + e));
@@ -473,12 +493,13 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_sums(DraftArgs a) {
 // registers between the sum and the search.
 constexpr int kMostSlices = 4 * kVerifyThreads;
 
-template <int KIND>
+// EACH: values of a slice in a thread.
+template <int KIND, int EACH>
 __global__ __launch_bounds__(kVerifyThreads) void k_verify_pick(DraftArgs a) {
-  constexpr int kSlices = kMostSlices / kVerifyThreads, kEach = kMaxDraftPart / kPartSlices / kVerifyThreads;
+  constexpr int kSlices = kMostSlices / kVerifyThreads, kEach = EACH;
   __shared__ double waves[2][2][kVerifyWaves];
   __shared__ Found found[2][kVerifyWaves];
-  __shared__ int32_t places[KIND == kDraftList ? kMaxDraftPart / kPartSlices : 1];
+  __shared__ __align__(16) int32_t places[KIND == kDraftList ? EACH * kVerifyThreads : 4];
   const int b = blockIdx.x, slices = a.parts * kPartSlices, slice = a.part_size / kPartSlices;
   const double2* part = reinterpret_cast<const double2*>(a.part) + (size_t)b * slices;
   double w[kSlices], whole[kSlices], sums[2] = {0.0, 0.0};
@@ -499,7 +520,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_pick(DraftArgs a) {
   for (int e = 0; e < kSlices; ++e) w[e] = nothing ? whole[e] : w[e];
   const double mark = sample * (nothing ? r.total[1] : r.total[0]);
   double start, unused;
-  const int at_slice = find_place<kSlices>(w, nothing ? r.before[1] : r.before[0], mark, found[0], &start);
+  const int at_slice = find_place(w, nothing ? r.before[1] : r.before[0], mark, found[0], &start);
   int next = -1;
   if (at_slice >= 0) {
     const int v0 = at_slice * slice, size = min(slice, a.vocab - v0), first = (int)threadIdx.x * kEach;
@@ -507,7 +528,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_pick(DraftArgs a) {
     const PartDraft<KIND> q = part_draft<KIND>(a, b, accepted, accepted < length && !nothing, v0, slice, places);
     double x[kEach], sum = 0.0;
     // neighbouring threads load neighbouring values; in the order of the places they go through LDS
-    __shared__ float staged[kMaxDraftPart / kPartSlices];
+    __shared__ float staged[EACH * kVerifyThreads];
     float pv[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) pv[i] = p[min((int)threadIdx.x + i * kVerifyThreads, size - 1)];
@@ -523,24 +544,29 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify_pick(DraftArgs a) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) sum += x[i];
     const Running in = running_sums(sum, 0.0, waves[1]);
-    next = find_place<kEach>(x, start + in.before[0], mark, found[1], &unused);
+    next = find_place(x, start + in.before[0], mark, found[1], &unused);
     if (next >= 0) next += v0;
   }
   write_tokens(a, b, accepted, next);
 }
 
+// Parts of a dense row: about a thousand workgroups over the batch, of at least 1024 tokens; the slices of all of them are
+// what the workgroup that picks holds.  With a draft's list a part's places lie in LDS, and parts of up to 4096 tokens leave room
+// for eight workgroups on a compute unit: 64 sequences of 2 tokens, 256000 in the vocabulary, 32.4 -> 26.6 us.
+constexpr int kListPart = 4096;
+bool small_parts(const DraftArgs& a) { return a.draft_idx && a.vocab <= kListPart * (kMostSlices / kPartSlices); }
+DraftParts draft_parts(const DraftArgs& a) {
+  int parts = 1024 / a.B;
+  parts = parts < 16 ? 16 : (parts > kMostSlices / kPartSlices ? kMostSlices / kPartSlices : parts);
+  int size = ((a.vocab + parts - 1) / parts + 1023) / 1024 * 1024;
+  const int most = small_parts(a) ? kListPart : kMaxDraftPart;
+  if (size > most) size = most;
+  return DraftParts{(a.vocab + size - 1) / size, size};
+}
+
 }  // namespace
 
-// Parts of a dense row: about a thousand workgroups over the batch, of at least 1024 tokens; the slices of all of them are
-// what the workgroup that picks holds.
-DraftParts draft_parts(int B, int vocab) {
-  int parts = 1024 / B;
-  parts = parts < 16 ? 16 : (parts > kMostSlices / kPartSlices ? kMostSlices / kPartSlices : parts);
-  int size = ((vocab + parts - 1) / parts + 1023) / 1024 * 1024;
-  if (size > kMaxDraftPart) size = kMaxDraftPart;
-  return DraftParts{(vocab + size - 1) / size, size};
-}
-size_t draft_part_bytes(int B, int vocab) { return (size_t)B * draft_parts(B, vocab).count * kPartSlices * 2 * sizeof(double); }
+size_t draft_part_bytes(const DraftArgs& a) { return (size_t)a.B * draft_parts(a).count * kPartSlices * 2 * sizeof(double); }
 
 hipError_t launch_verify(DraftArgs a, hipStream_t s) {
   if (a.target_idx) {
@@ -549,22 +575,35 @@ hipError_t launch_verify(DraftArgs a, hipStream_t s) {
       const dim3 grid((unsigned)a.B), block((unsigned)(kWave * (a.n + 1)));
       return longest <= kWave ? launch(&k_verify_short<1>, grid, block, 0, s, a) : launch(&k_verify_short<kShortEach>, grid, block, 0, s, a);
     }
-    const dim3 grid((unsigned)a.B), block(kVerifyThreads);
-    if (longest <= 2 * kVerifyThreads) return launch(&k_verify_lists<2>, grid, block, 0, s, a);
-    return launch(longest <= 4 * kVerifyThreads ? &k_verify_lists<4> : &k_verify_lists<kMaxDraftList / kVerifyThreads>, grid, block, 0,
-                  s, a);
+    const dim3 grid((unsigned)a.B);
+    if (longest <= 512) return launch(&k_verify_lists<512, 1>, grid, dim3(512), 0, s, a);
+    if (longest <= 1024) return launch(&k_verify_lists<1024, 1>, grid, dim3(1024), 0, s, a);
+    return launch(&k_verify_lists<1024, kMaxDraftList / 1024>, grid, dim3(1024), 0, s, a);
   }
-  const DraftParts parts = draft_parts(a.B, a.vocab);
+  const DraftParts parts = draft_parts(a);
   a.parts = parts.count;
   a.part_size = parts.size;
   const bool vec = a.vocab % 4 == 0 && reinterpret_cast<uintptr_t>(a.target) % 16 == 0 &&
                    (!a.draft || a.draft_idx || reinterpret_cast<uintptr_t>(a.draft) % 16 == 0);
   auto both = [&](auto kind) {
     constexpr int KIND = decltype(kind)::value;
-    const dim3 grid((unsigned)a.parts, (unsigned)a.B);
-    const hipError_t e = vec ? launch(&k_verify_sums<KIND, true>, grid, dim3(kVerifyThreads), 0, s, a)
-                             : launch(&k_verify_sums<KIND, false>, grid, dim3(kVerifyThreads), 0, s, a);
-    return e != hipSuccess ? e : launch(&k_verify_pick<KIND>, dim3((unsigned)a.B), dim3(kVerifyThreads), 0, s, a);
+    auto sums = [&](auto part) {
+      constexpr int PART = decltype(part)::value;
+      const dim3 grid((unsigned)a.parts, (unsigned)a.B);
+      return vec ? launch(&k_verify_sums<KIND, true, PART>, grid, dim3(kVerifyThreads), 0, s, a)
+                 : launch(&k_verify_sums<KIND, false, PART>, grid, dim3(kVerifyThreads), 0, s, a);
+    };
+    hipError_t e;
+    if constexpr (KIND == kDraftList)
+      e = small_parts(a) ? sums(std::integral_constant<int, kListPart>{}) : sums(std::integral_constant<int, kMaxDraftPart>{});
+    else
+      e = sums(std::integral_constant<int, 0>{});
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)a.B), block(kVerifyThreads);
+    const int each = a.part_size / kPartSlices / kVerifyThreads;  // at least one: a part is whole thousands
+    if (each <= 1) return launch(&k_verify_pick<KIND, 1>, grid, block, 0, s, a);
+    if (each <= 4) return launch(&k_verify_pick<KIND, 4>, grid, block, 0, s, a);
+    return launch(&k_verify_pick<KIND, kMaxDraftPart / kPartSlices / kVerifyThreads>, grid, block, 0, s, a);
   };
   if (!a.draft) return both(std::integral_constant<int, kDraftCertain>{});
   if (!a.draft_idx) return both(std::integral_constant<int, kDraftDense>{});
