@@ -520,6 +520,9 @@ struct MxProduct {
 };
 size_t mx_workspace_bytes(int T, int rows, int cols);
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s);
+// mxfp4_stream.hip: many rows of whole 512 columns, their scale bytes 16-byte aligned, with a few tokens; parts: of the columns.
+int mx_stream_parts(int cols);
+hipError_t launch_mx_stream(const MxProduct& p, hipStream_t s);
 
 // ---- verify.hip: drafted tokens against the target's probabilities ----------------
 constexpr int kMaxDraft = 63;          // drafted tokens of a sequence: with the one behind them a wave's lanes

@@ -30,4 +30,35 @@ __device__ __forceinline__ uint4 mx_to_bf16(uint32_t codes, float scale) {
   return u;
 }
 
+// Lane (row r, q = lane / 16) has sixteen bytes of codes, block q of four; afterwards word j of it is word q of block j.
+template <int RU>
+__device__ __forceinline__ void exchange_blocks(uint4 (&c)[RU]) {
+#pragma unroll
+  for (int r = 0; r < RU; ++r) {
+    const auto a = __builtin_amdgcn_permlane32_swap(c[r].x, c[r].z, false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(c[r].y, c[r].w, false, false);
+    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    c[r] = make_uint4(lo[0], lo[1], hi[0], hi[1]);
+  }
+}
+
+// Four neighbouring rows' results of a token, as far as they are there.
+__device__ __forceinline__ void store_rows(void* __restrict__ y, int y_bf16, int T, int rows, int token, int row, const f32x4v& v) {
+  if (token >= T || row >= rows) return;
+  const size_t at = (size_t)token * rows + row;
+  if (rows % 4 != 0) {
+    for (int e = 0; e < 4 && row + e < rows; ++e) {
+      if (y_bf16)
+        static_cast<__bf16*>(y)[at + e] = (__bf16)v[e];
+      else
+        static_cast<float*>(y)[at + e] = v[e];
+    }
+  } else if (y_bf16) {
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(y) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
 }  // namespace hire

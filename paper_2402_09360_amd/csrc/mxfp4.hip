@@ -59,17 +59,6 @@ __global__ __launch_bounds__(256) void k_unpack_mxfp4(const uint32_t* __restrict
 //   bf16 tokens: one instruction per block, whose lane holds columns 8 q ... of the block; so the four lanes of a row first
 // exchange words, after which word q of block j is word j of lane q.  Then sixteen bytes of a token are 64 in a row of four
 // lanes; of a lane's own block they would be 16 bytes every 64.
-template <int RU>
-__device__ __forceinline__ void exchange_blocks(uint4 (&c)[RU]) {
-#pragma unroll
-  for (int r = 0; r < RU; ++r) {
-    const auto a = __builtin_amdgcn_permlane32_swap(c[r].x, c[r].z, false, false);
-    const auto b = __builtin_amdgcn_permlane32_swap(c[r].y, c[r].w, false, false);
-    const auto lo = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
-    const auto hi = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    c[r] = make_uint4(lo[0], lo[1], hi[0], hi[1]);
-  }
-}
 // The four scale bytes of blocks 4 s ... of a row; behind the last one: 127 (the codes there are zeros).
 __device__ __forceinline__ uint32_t scale_word(const uint8_t* row, int s, int blocks, bool words) {
   if (words) return reinterpret_cast<const uint32_t*>(row)[s];
@@ -438,27 +427,12 @@ __global__ __launch_bounds__(64 * RW * KW) void k_mx_shared(const uint8_t* __res
       for (int t = 0; t < NT; ++t) acc[r][t] += join[(r * NT + t) * 64];
   }
   // acc[r][t]: token 16 t + lane % 16, rows 16 r + 4 (lane / 16) ...
-  float* out = static_cast<float*>(y);
 #pragma unroll
   for (int r = 0; r < RU; ++r)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int token = 16 * t + (lane & 15), n = row0 + 16 * r + 4 * q;
-      if (token >= T || n >= rows) continue;
-      const size_t at = (size_t)token * rows + n;
-      const f32x4v v = acc[r][t];
-      if (rows % 4 != 0) {
-        for (int e = 0; e < 4 && n + e < rows; ++e) {
-          if (y_bf16)
-            static_cast<__bf16*>(y)[at + e] = (__bf16)v[e];
-          else
-            out[at + e] = v[e];
-        }
-      } else if (y_bf16) {
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(y) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-      } else {
-        *reinterpret_cast<float4*>(out + at) = make_float4(v[0], v[1], v[2], v[3]);
-      }
+      store_rows(y, y_bf16, T, rows, token, n, acc[r][t]);
     }
 }
 
@@ -627,19 +601,38 @@ size_t mx_padded_bytes(int T, int rows, int cols) {
 // of 8192 columns 28.2 / 12.7, on 8192 rows 30.5 / 19.9; 1000 on 1024 of 8192 28.2 / 23.3; 128 on 2048 of 4096 16.5 / 11.7.  Every
 // other tile and number of parts was timed for 16 such sizes: at most 9 % better.
 ProductShape mx_shape(int T, int rows, int cols) { return product_shape(T, rows, (cols + 127) / 128, 1, 32); }
+// Rows streamed past the tokens (mxfp4_stream.hip): matrices that keep every compute unit at it for a while.  us without / with it:
+//   bf16, two / sixteen tokens: 4096 rows of 4096 columns 6.1, 5.5 / 8.3, 7.4, of 1024 3.7, 4.9 / 4.3, 6.9 (no), 8192 of 2048 5.3,
+// 5.5 / 6.8, 7.2, 256000 of 2048 66.8, 61.2 / 72.4, 58.6, 12000 of 8192 23.8, 18.2 / 32.4, 20.1; rows in parts (more than 4096
+// columns) pay later: 4096 of 8192 9.6, 10.0 / 13.8, 12.2.  20: 12000 of 8192 31.7, 25.9, 65536 of 2048 23.5, 27.5 (no).
+//   packed, one / sixteen: 8192 of 2048 5.0, 4.8 / 6.0, 5.3, of 1024 4.0, 4.4 / 4.6, 5.1 (no), 16384 of 16384 45.7, 30.0 / 49.9,
+// 31.8; 20: 8192 of 1024 6.6, 5.8, 4096 of 1024 5.0, 5.6 (no); 48 / 64: 8192 of 4096 15.8, 11.2 / 18.3, 13.2, 20000 of 8192 31.7,
+// 28.4 / 34.1, 31.6, but 65536 of 2048 20.9, 23.0 / 22.2, 25.7 (no: tiles).
+bool mx_streams(int T, int rows, int cols, bool packed) {
+  if (cols % 512 != 0 || cols < 1024 || T > (packed ? kMxFewTokens : 32) || (T == 1 && !packed)) return false;
+  const long long values = (long long)rows * cols;
+  if (T <= 16) return values >= 1 << 24 && (mx_stream_parts(cols) == 1 || T > 8 || values > 1 << 26);
+  if (!packed) return cols >= 4096 && values >= 1 << 26;
+  return values >= 1 << 23 && (T <= 32 || rows < 16384 || cols >= 4096);
+}
 size_t mx_parts_bytes(int splits, int T, int rows) { return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0; }
 }  // namespace
 
-// Room for the parts of the sums and, with tiles, for padded scale bytes in front of them, whichever the call needs.
+// Room for the parts of the sums and, with tiles, for padded scale bytes in front of them, whichever a call of this size needs.
 size_t mx_workspace_bytes(int T, int rows, int cols) {
   const size_t tiles =
       mx_tiles(T, rows) ? mx_padded_bytes(T, rows, cols) + mx_parts_bytes(mx_shape(T, rows, cols).splits, T, rows) : 0;
   if (T > kMxFewTokens) return tiles;
-  const size_t parts = mx_parts_bytes(few_splits(T, rows, cols), T, rows);
+  // a call's alignment and tokens may allow the rows to be streamed or not
+  const int splits = few_splits(T, rows, cols), streams = mx_streams(T, rows, cols, true) || mx_streams(T, rows, cols, false)
+                                                              ? mx_stream_parts(cols) : 1;
+  const size_t parts = mx_parts_bytes(splits > streams ? splits : streams, T, rows);
   return parts > tiles ? parts : tiles;
 }
 
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s) {
+  if (mx_streams(p.T, p.rows, p.cols, p.x_scales != nullptr) && reinterpret_cast<uintptr_t>(p.scales) % 16 == 0)
+    return launch_mx_stream(p, s);
   if (!p.x_scales) return launch_few_tokens<false>(p, s);
   if (!mx_tiles(p.T, p.rows)) return launch_few_tokens<true>(p, s);
   const int blocks = p.cols / kMxBlock, words = (blocks + 15) / 16 * 4;

@@ -1,0 +1,195 @@
+// Product of many packed rows with a few tokens: bound by reading the rows once.
+//   A wave keeps what it needs of the tokens in registers for as long as it lives, 1024 columns of them, and works on sixteen rows
+// of these columns after the other.  The codes come to LDS by asynchronous loads of whole runs of 512 bytes, three sixteens ahead
+// (34 KB on their way for each of the four waves of a compute unit), without a barrier: every wave has its own places.  SPAN waves
+// share rows of up to 1024 SPAN columns and add their sums; longer rows are split into parts.  Against tokens that come from the L2
+// or LDS and codes that come to registers one step ahead, in pieces of 64 bytes: 60000 rows of 8192 columns, two bf16 tokens 71 ->
+// 56 us, sixteen 83 -> 59 (4.5 TB/s), sixteen packed ones 73 -> 57.
+#include "mxfp4.h"
+
+#include "dense_epilogue.h"
+
+namespace hire {
+namespace {
+
+constexpr int kStreamWaves = 4, kStreamCols = 1024, kStreamSteps = kStreamCols / 128, kStreamPlaces = 4;
+constexpr int kStreamCodes = 16 * kStreamCols / 2, kStreamScales = 16 * kStreamCols / kMxBlock;
+constexpr int kStreamPlace = kStreamCodes + kStreamScales;
+constexpr int kStreamLoads = kStreamCodes / 1024 + 1;  // of a place
+
+template <bool PACKED, int NT, int SPAN>
+__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_mx_stream(
+    const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const void* __restrict__ x,
+    const uint8_t* __restrict__ x_scales, int T, int rows, int cols, int part_cols, void* __restrict__ y, int y_bf16,
+    float* __restrict__ part) {
+  constexpr int kGroups = kStreamWaves / SPAN;  // sixteens of rows at a time
+  __shared__ __align__(1024) char smem[kStreamWaves * kStreamPlaces * kStreamPlace];
+  __shared__ f32x4v join[SPAN > 1 ? kStreamWaves * NT * 64 : 1];
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, q = lane >> 4;
+  const int in_span = wave % SPAN, blocks = cols / kMxBlock;
+  const int col_end = min(((int)blockIdx.y + 1) * part_cols, cols), col0 = (int)blockIdx.y * part_cols + in_span * kStreamCols;
+  const int there = max(col_end - col0, 0) / kMxBlock;  // blocks of this wave, a multiple of sixteen
+
+  // the tokens
+  uint4 xv[NT][kStreamSteps][PACKED ? 1 : 4];
+  uint32_t xs[NT][PACKED ? kStreamSteps : 1];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const size_t token = (size_t)min(16 * t + r, T - 1);
+#pragma unroll
+    for (int s = 0; s < kStreamSteps; ++s) {
+      const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (PACKED) {
+        const bool in = 4 * s + q < there;
+        const size_t block = token * blocks + (in ? col0 / kMxBlock + 4 * s + q : 0);
+        const uint4 v = reinterpret_cast<const uint4*>(x)[block];
+        xv[t][s][0] = in ? v : zeros;
+        xs[t][s] = in ? x_scales[block] : 127u;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool in = 4 * s + j < there;
+          const uint4 v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + token * cols +
+                                                         (in ? col0 + (4 * s + j) * kMxBlock : 0))[q];
+          xv[t][s][j] = in ? v : zeros;
+        }
+      }
+    }
+  }
+
+  const int groups = (rows + 15) / 16, batches = (groups + kGroups - 1) / kGroups;
+  const int n = (batches - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;  // at least one
+  auto row_of = [&](int i) { return (((int)blockIdx.x + i * (int)gridDim.x) * kGroups + wave / SPAN) * 16; };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem)) + (uint32_t)wave * kStreamPlaces * kStreamPlace;
+  const uint32_t ld = (uint32_t)cols / 2;
+  // A load is two rows; the sixteen bytes c of row r lie at c ^ r.  Blocks behind the last one are read as zeros.
+  auto request = [&](int i) __attribute__((always_inline)) {
+    const int row0 = min(row_of(i), rows - 1), last = rows - 1 - row0;
+    const uint32_t lds = lds0 + (uint32_t)(i % kStreamPlaces) * kStreamPlace;
+    const char* base = reinterpret_cast<const char*>(codes) + (size_t)row0 * ld + col0 / 2;
+#pragma unroll
+    for (int p = 0; p < kStreamCodes / 1024; ++p) {
+      const int row = 2 * p + (lane >> 5), chunk = (lane & 31) ^ row;
+      const uint32_t off = (uint32_t)min(row, last) * ld + (uint32_t)chunk * 16;
+      if (there == kStreamCols / kMxBlock)
+        gemm_load(base, off, lds + p * 1024);
+      else
+        gemm_load_at(chunk < there ? (const void*)(base + off) : (const void*)kGemmZeros, lds + p * 1024);
+    }
+    if (lane < kStreamScales / 16) {  // sixteen bytes, two a row
+      const int row = min(lane >> 1, last), half = lane & 1;
+      const uint8_t* from = scales + (size_t)(row0 + row) * blocks + col0 / kMxBlock + 16 * half;
+      gemm_load_at(16 * half < there ? (const void*)from : (const void*)kGemmZeros, lds + kStreamCodes);
+    }
+  };
+  for (int i = 0; i < kStreamPlaces - 1 && i < n; ++i) request(i);
+  for (int i = 0; i < n; ++i) {
+    if (i + 2 < n)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kStreamLoads) : "memory");
+    else if (i + 1 < n)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStreamLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    const char* place = smem + (wave * kStreamPlaces + i % kStreamPlaces) * kStreamPlace;
+    uint32_t sc[kStreamSteps];
+    *reinterpret_cast<uint4*>(&sc[0]) = *reinterpret_cast<const uint4*>(place + kStreamCodes + r * 32);
+    *reinterpret_cast<uint4*>(&sc[4]) = *reinterpret_cast<const uint4*>(place + kStreamCodes + r * 32 + 16);
+    f32x4v acc[NT] = {};
+#pragma unroll
+    for (int s = 0; s < kStreamSteps; ++s) {
+      uint4 c[1] = {*reinterpret_cast<const uint4*>(place + r * (kStreamCols / 2) + (((4 * s + q) ^ r) << 4))};
+      if constexpr (PACKED) {
+        const i32x8v cv = {(int)c[0].x, (int)c[0].y, (int)c[0].z, (int)c[0].w, 0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const i32x8v tv = {(int)xv[t][s][0].x, (int)xv[t][s][0].y, (int)xv[t][s][0].z, (int)xv[t][s][0].w, 0, 0, 0, 0};
+          acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(cv, tv, acc[t], 4, 4, 0, (int)(sc[s] >> (8 * q)), 0,
+                                                                    (int)xs[t][s]);
+        }
+      } else {
+        exchange_blocks<1>(c);
+        auto block = [&](auto which, uint32_t word) {
+          constexpr int J = decltype(which)::value;
+          const uint4 w4 = mx_to_bf16(word, mx_scale_of<J>(sc[s]));
+          bf16x8v wv;
+          __builtin_memcpy(&wv, &w4, 16);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            bf16x8v xf;
+            __builtin_memcpy(&xf, &xv[t][s][J], 16);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xf, acc[t], 0, 0, 0);
+          }
+        };
+        block(std::integral_constant<int, 0>{}, c[0].x);
+        block(std::integral_constant<int, 1>{}, c[0].y);
+        block(std::integral_constant<int, 2>{}, c[0].z);
+        block(std::integral_constant<int, 3>{}, c[0].w);
+      }
+    }
+    // Every lane takes part in the instructions above, also those that store nothing below: without this the compiler moves the
+    // scaled ones and the reads in front of them behind that condition.
+#pragma unroll
+    for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(acc[t]));
+    if (i + kStreamPlaces - 1 < n) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      request(i + kStreamPlaces - 1);
+    }
+    // acc[t]: token 16 t + lane % 16, rows 4 q ... of the sixteen
+    auto store = [&](int t, int from, const f32x4v& v) __attribute__((always_inline)) {
+      store_rows(gridDim.y > 1 ? part + (size_t)blockIdx.y * T * rows : y, gridDim.y > 1 ? 0 : y_bf16, T, rows,
+                 16 * t + (from & 15), row_of(i) + 4 * (from >> 4), v);
+    };
+    if constexpr (SPAN == 1) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) store(t, lane, acc[t]);
+    } else {
+      if (i > 0) lds_barrier();  // the sums before are read
+#pragma unroll
+      for (int t = 0; t < NT; ++t) join[(wave * NT + t) * 64 + lane] = acc[t];
+      lds_barrier();
+      for (int t = in_span; t < NT; t += SPAN) {
+        const f32x4v* first = join + ((wave - in_span) * NT + t) * 64 + lane;
+        f32x4v v = first[0];
+#pragma unroll
+        for (int w = 1; w < SPAN; ++w) v += first[w * NT * 64];
+        store(t, lane, v);
+      }
+    }
+  }
+}
+
+template <bool PACKED, int NT, int SPAN>
+hipError_t launch_stream(const MxProduct& p, int parts, int part_cols, hipStream_t s) {
+  const int batches = (p.rows + 16 * (kStreamWaves / SPAN) - 1) / (16 * (kStreamWaves / SPAN)), each = 256 / parts;
+  float* part = static_cast<float*>(p.workspace);
+  const hipError_t e = launch(&k_mx_stream<PACKED, NT, SPAN>, dim3((unsigned)(batches < each ? batches : each), (unsigned)parts),
+                              dim3(64 * kStreamWaves), 0, s, p.codes, p.scales, p.x, p.x_scales, p.T, p.rows, p.cols, part_cols, p.y,
+                              p.y_bf16, part);
+  if (e != hipSuccess || parts == 1) return e;
+  return launch_join_parts(part, p.y, p.y_bf16 != 0, parts, (long long)p.T * p.rows, s);
+}
+template <bool PACKED, int NT>
+hipError_t launch_by_columns(const MxProduct& p, hipStream_t s) {
+  const int parts = mx_stream_parts(p.cols), part_cols = (p.cols / 512 + parts - 1) / parts * 512;
+  if (part_cols <= kStreamCols) return launch_stream<PACKED, NT, 1>(p, parts, part_cols, s);
+  if (part_cols <= 2 * kStreamCols) return launch_stream<PACKED, NT, 2>(p, parts, part_cols, s);
+  return launch_stream<PACKED, NT, 4>(p, parts, part_cols, s);
+}
+
+}  // namespace
+
+int mx_stream_parts(int cols) { return (cols + 4 * kStreamCols - 1) / (4 * kStreamCols); }
+
+hipError_t launch_mx_stream(const MxProduct& p, hipStream_t s) {
+  const int tiles = (p.T + 15) / 16;
+  if (p.x_scales) {
+    if (tiles == 1) return launch_by_columns<true, 1>(p, s);
+    if (tiles == 2) return launch_by_columns<true, 2>(p, s);
+    if (tiles == 3) return launch_by_columns<true, 3>(p, s);
+    return launch_by_columns<true, 4>(p, s);
+  }
+  if (tiles == 1) return launch_by_columns<false, 1>(p, s);
+  return launch_by_columns<false, 2>(p, s);
+}
+
+}  // namespace hire

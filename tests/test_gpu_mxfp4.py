@@ -182,6 +182,38 @@ def test_products_in_parts(hire, T, rows, cols, dtype):
     product_case(hire, T, rows, cols, True, dtype)
 
 
+@pytest.mark.parametrize("rows,cols", [(16397, 1024), (10923, 1536), (8205, 2048), (5001, 4096), (8200, 8192), (13500, 5120)])
+@pytest.mark.parametrize("T,packed", [(2, False), (9, False), (16, False), (31, False), (1, True), (16, True), (32, True), (47, True),
+                                      (64, True)])
+def test_streamed_rows(hire, T, packed, rows, cols):
+    print(f"T={T} {rows}x{cols} packed={packed}", flush=True)
+    product_case(hire, T, rows, cols, packed, torch.float32 if T % 2 else torch.bfloat16)
+
+
+def test_scales_that_start_anywhere(hire):
+    """The same results, up to the order of the sums, from scale bytes at any address."""
+    rows, cols = 5000, 4096
+    wq = hire.hire_pack_mxfp4(matrix(1, rows, cols))
+    wv = hire.hire_unpack_mxfp4(wq).double()
+    for T, packed in ((3, False), (20, False), (64, False), (3, True), (30, True), (64, True), (100, True)):
+        x = matrix(T, T, cols)
+        xq = hire.hire_pack_mxfp4(x)
+        xv = hire.hire_unpack_mxfp4(xq).double() if packed else x.double()
+        want, room = xv @ wv.t(), 2.02 * (cols + 8) * 2.0 ** -24 * (xv.abs() @ wv.abs().t())
+        for at in (0, 1, 4, 8):
+            def moved(q):
+                buffer = torch.zeros(q.scales.numel() + 16, dtype=torch.uint8, device="cuda")
+                buffer[at:at + q.scales.numel()] = q.scales.flatten()
+                return hire.Mxfp4(q.codes, buffer[at:at + q.scales.numel()].view(q.scales.shape))
+            y = torch.empty((T, rows), device="cuda")
+            ws = hire.alloc_workspace(hire.hire_mxfp4_product_workspace_bytes(T, rows, cols))
+            if packed:
+                hire.hire_mxfp4_product(moved(xq), moved(wq), y, ws)
+            else:
+                hire.hire_mxfp4_product_bf16(x, moved(wq), y, ws)
+            assert bool(((y.double() - want).abs() <= room).all()), (T, packed, at)
+
+
 @pytest.mark.parametrize("rows,cols", [(40000, 256), (33000, 96), (3, 65536)])
 def test_long_matrices(hire, rows, cols):
     for T, packed in ((1, False), (1, True), (20, False), (64, False), (50, True)):
