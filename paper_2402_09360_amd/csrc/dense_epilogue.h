@@ -89,6 +89,7 @@ struct StorePart {
 __device__ __forceinline__ void join_eight(const float* part, int parts, size_t stride, float (&v)[8]) {
   const float4 a = reinterpret_cast<const float4*>(part)[0], b = reinterpret_cast<const float4*>(part)[1];
   v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+#pragma unroll 4
   for (int r = 1; r < parts; ++r) {
     const float4* p = reinterpret_cast<const float4*>(part + r * stride);
     const float4 c = p[0], d = p[1];
@@ -113,6 +114,7 @@ __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ pa
   if (values % 4 != 0) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < values; i += (long long)gridDim.x * 256) {
       float s = part[i];
+#pragma unroll 8
       for (int r = 1; r < parts; ++r) s += part[(size_t)r * values + i];
       if constexpr (BF16)
         static_cast<__bf16*>(out)[i] = (__bf16)s;
@@ -125,6 +127,7 @@ __global__ __launch_bounds__(256) void k_join_parts(const float* __restrict__ pa
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < quads; i += (long long)gridDim.x * 256) {
     const float4* p = reinterpret_cast<const float4*>(part) + i;
     float4 s = p[0];
+#pragma unroll 8
     for (int r = 1; r < parts; ++r) {
       const float4 v = p[(size_t)r * quads];
       s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;

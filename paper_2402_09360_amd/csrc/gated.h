@@ -46,6 +46,37 @@ __device__ __forceinline__ void unpack_kept(const uint4& g, const uint4& u, cons
   }
 }
 
+// h = a(g) u of eight units, and what the backward pass needs (kept.g null: h only).
+template <int ACT>
+__device__ __forceinline__ void store_gated(const GatedKept& kept, size_t at, const float (&g)[8], const float (&u)[8]) {
+  float hv[8], slope;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) hv[e] = activation<ACT>(g[e], &slope) * u[e];
+  *reinterpret_cast<uint4*>(kept.h + at) = pack8(hv);
+  if (kept.g) {
+    uint32_t gd[4], ud[4], low[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      gd[q] = upper_pair(g[2 * q], g[2 * q + 1]);
+      ud[q] = upper_pair(u[2 * q], u[2 * q + 1]);
+      low[q] = lower_pair(g[2 * q], u[2 * q], g[2 * q + 1], u[2 * q + 1]);
+    }
+    *reinterpret_cast<uint4*>(kept.g + at) = make_uint4(gd[0], gd[1], gd[2], gd[3]);
+    *reinterpret_cast<uint4*>(kept.u + at) = make_uint4(ud[0], ud[1], ud[2], ud[3]);
+    *reinterpret_cast<uint4*>(kept.low + at) = make_uint4(low[0], low[1], low[2], low[3]);
+  }
+}
+// The same from parts of k (StorePart<true>'s order).
+template <int ACT>
+__global__ __launch_bounds__(256) void k_join_gated(const float* __restrict__ part, int parts, long long values, GatedKept kept) {
+  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < values; i += (long long)gridDim.x * 2048) {
+    float g[8], u[8];
+    join_eight(part + i, parts, 2 * (size_t)values, g);
+    join_eight(part + values + i, parts, 2 * (size_t)values, u);
+    store_gated<ACT>(kept, (size_t)i, g, u);
+  }
+}
+
 // Calls f with the activation as a type.
 template <typename F>
 hipError_t with_activation(int act, F f) {

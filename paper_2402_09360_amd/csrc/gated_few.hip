@@ -291,6 +291,8 @@ __global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(DownPairs from, 
   }
 }
 
+constexpr int kMostStreamParts = 8;
+
 // Parts of the rows: about 512 workgroups, of at least one block of 32 rows per wave.
 int down_parts(int d, int rows) {
   const int columns = (d + 127) / 128, most = (rows + 32 * kDownWaves - 1) / (32 * kDownWaves);
@@ -411,9 +413,15 @@ hipError_t launch_down(const DownPairs& from, int T, int d, int d_ff, uint16_t* 
   return launch_join_parts(part, out, true, parts, (long long)T * d, s);
 }
 
+// The first layer's rows streamed past the tokens (gated_stream.hip): where they keep every compute unit at it for a while.  us of
+// both layers without / with it, 17 / 48 tokens: d = 2048, 16384 units 52.3, 51.2 / 59.7, 54.8; 2560, 10240 66.5, 49.8 / 80.5,
+// 57.1; 8192, 8192 93.9, 89.2 / 122, 98; 1024, 8192 24.7, 24.6 / 29.5, 28.0; not 1024, 4096 18.3, 19.4 / 22.5, 24.3 or 512, 8192 20.6,
+// 22.6 / 23.4, 26.6.
+bool few_streams(int d, int d_ff) { return d >= 1024 && (long long)d * d_ff >= 1 << 23 && gated_stream_parts(d) <= kMostStreamParts; }
+
 template <int NT, int RU>
 hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
-  const hipError_t e = with_activation(L.act, [&](auto act) {
+  const hipError_t e = few_streams(L.d, L.d_ff) ? launch_gated_stream(L, x, T, kept, part, s) : with_activation(L.act, [&](auto act) {
     return launch(&k_gated_up<decltype(act)::value, NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
                   dim3(64 * kUpWaves), 0, s, L, x, T, kept);
   });
@@ -459,8 +467,10 @@ hipError_t launch_few_by_width(const GatedLayer& L, const uint16_t* x, int T, ui
 
 size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs) {
   if (pairs == 1 && one_kernel(T, d, d_ff)) return (size_t)one_parts(d_ff) * T * d * sizeof(float);
-  const int parts = down_parts(d, pairs * d_ff);
-  return parts > 1 ? (size_t)parts * T * d * sizeof(float) : 0;
+  const int parts = down_parts(d, pairs * d_ff), streams = pairs == 1 && few_streams(d, d_ff) ? gated_stream_parts(d) : 1;
+  const size_t down = parts > 1 ? (size_t)parts * T * d * sizeof(float) : 0;
+  const size_t up = streams > 1 ? 2 * (size_t)streams * T * d_ff * sizeof(float) : 0;
+  return down > up ? down : up;
 }
 
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,

@@ -498,6 +498,9 @@ constexpr int kGatedFewTokens = 64;
 size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs);  // pairs: 1 forward, 2 dx
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                             hipStream_t s);
+// gated_stream.hip: the first layer alone, in so many parts of d
+int gated_stream_parts(int d);
+hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s);
 hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
                                    hipStream_t s);
 hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
     for (int p = 0; p < kStreamCodes / 1024; ++p) {
       const int row = 2 * p + (lane >> 5), chunk = (lane & 31) ^ row;
       const uint32_t off = (uint32_t)min(row, last) * ld + (uint32_t)chunk * 16;
-      if (there == kStreamCols / kMxBlock)
+      if (there >= kStreamCols / kMxBlock)
         gemm_load(base, off, lds + p * 1024);
       else
         gemm_load_at(chunk < there ? (const void*)(base + off) : (const void*)kGemmZeros, lds + p * 1024);
@@ -85,11 +85,12 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
   for (int i = 0; i < kStreamPlaces - 1 && i < n; ++i) request(i);
   for (int i = 0; i < n; ++i) {
     if (i + 2 < n)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kStreamLoads) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kStreamLoads) : "memory");
     else if (i + 1 < n)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStreamLoads) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kStreamLoads) : "memory");
     else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (i + kStreamPlaces - 1 < n) request(i + kStreamPlaces - 1);  // where the sixteen before had theirs
     const char* place = smem + (wave * kStreamPlaces + i % kStreamPlaces) * kStreamPlace;
     uint32_t sc[kStreamSteps];
     *reinterpret_cast<uint4*>(&sc[0]) = *reinterpret_cast<const uint4*>(place + kStreamCodes + r * 32);
@@ -130,10 +131,6 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
     // scaled ones and the reads in front of them behind that condition.
 #pragma unroll
     for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(acc[t]));
-    if (i + kStreamPlaces - 1 < n) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      request(i + kStreamPlaces - 1);
-    }
     // acc[t]: token 16 t + lane % 16, rows 4 q ... of the sixteen
     auto store = [&](int t, int from, const f32x4v& v) __attribute__((always_inline)) {
       store_rows(gridDim.y > 1 ? part + (size_t)blockIdx.y * T * rows : y, gridDim.y > 1 ? 0 : y_bf16, T, rows,

@@ -132,6 +132,16 @@ def test_products_in_parts(hire, T, d, F, act):
     check(run(hire, data, act), data, act)
 
 
+@pytest.mark.parametrize("T,d,F,act", [
+    (17, 1024, 8200, "silu"), (40, 2056, 4104, "gelu"), (64, 3000, 2808, "silu"), (33, 5000, 1688, "gelu"),
+    (48, 16384, 520, "silu"), (12, 8192, 4104, "gelu"), (16, 2048, 16384, "silu"), (31, 1032, 8136, "gelu")])
+def test_few_tokens_of_large_layers(hire, T, d, F, act):
+    print(f"T={T} d={d} F={F} {act}", flush=True)
+    data = inputs(T + d, T, d, F)
+    check(run(hire, data, act), data, act)
+    assert torch.equal(run(hire, data, act, train=False)["y"], run(hire, data, act)["y"])
+
+
 @pytest.mark.parametrize("T,d,F", [(1, 64, 128), (40, 96, 264), (130, 64, 512), (300, 128, 136)])
 def test_relu_at_zero(hire, T, d, F):
     """Exact pre-activations, some of them 0 (of 128 with one token none is): the slope there is 0."""
