@@ -196,109 +196,15 @@ __device__ __forceinline__ void mask_rows(int row0, int end, uint4 (&rows)[8]) {
     if (first + r >= end) rows[r] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-constexpr int kDownWaves = 8;
-
-// Columns 128 blockIdx.x ..., rows of part blockIdx.y: the waves take blocks of 32 rows in turn, of the second pair of matrix and
-// values behind those of the first (dx; a pair only: y).  The parts' sums are joined by k_join_parts; one part only: the result
-// itself.
-struct DownPairs {
-  const uint16_t *w[2], *h[2];
-  int pairs;
-};
-template <int NT>
-__global__ __launch_bounds__(64 * kDownWaves) void k_gated_down(DownPairs from, int T, int d, int d_ff, float* __restrict__ part,
-                                                                uint16_t* __restrict__ y) {
-  __shared__ float red[kDownWaves * 2048];
-  const int lane = lane_id(), wave = wave_id(), parts = gridDim.y, each = (d_ff + 31) / 32, blocks = each * from.pairs;
-  const int b0 = (int)((long long)blocks * blockIdx.y / parts), b1 = (int)((long long)blocks * (blockIdx.y + 1) / parts);
-  const int chunk = min((int)blockIdx.x * 16 + (lane & 15), d / 8 - 1);
-  size_t token[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) token[t] = (size_t)min(16 * t + (lane & 15), T - 1) * d_ff;
-  f32x4v acc[NT][8] = {};
-  auto load = [&](int block, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
-    const int pair = block >= each ? 1 : 0, b = block - pair * each;  // uniform
-    load_rows(from.w[pair], d, chunk, 32 * b, d_ff, rows);
-    const uint16_t* h = from.h[pair] + min(32 * b + 8 * (lane >> 4), d_ff - 8);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) hv[t] = *reinterpret_cast<const uint4*>(h + token[t]);
-  };
-  auto multiply = [&](int block, uint4 (&rows)[8], uint4 (&hv)[NT]) __attribute__((always_inline)) {
-    const int b = block >= each ? block - each : block;
-    if (32 * b + 32 > d_ff) {  // uniform; d_ff is a multiple of 8, so a lane's eight rows are there or not as a whole
-      mask_rows(32 * b, d_ff, rows);
-      if (32 * b + 8 * (lane >> 4) >= d_ff) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) hv[t] = make_uint4(0u, 0u, 0u, 0u);
-      }
-    }
-    bf16x8v hf[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) __builtin_memcpy(&hf[t], &hv[t], 16);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const bf16x8v col = column_of(rows, c);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hf[t], col, acc[t][c], 0, 0, 0);
-    }
-  };
-  uint4 ra[8], ha[NT];
-  int b = b0 + wave;
-  if constexpr (NT > 2) {  // the sums take half of the registers: one block at a time
-    for (; b < b1; b += kDownWaves) {
-      load(b, ra, ha);
-      multiply(b, ra, ha);
-    }
-  } else if (b < b1) {
-    uint4 rb[8], hb[NT];
-    load(b, ra, ha);
-    for (; b + kDownWaves < b1; b += 2 * kDownWaves) {
-      load(b + kDownWaves, rb, hb);
-      multiply(b, ra, ha);
-      load(min(b + 2 * kDownWaves, blocks - 1), ra, ha);  // not used where it repeats the last block
-      multiply(b + kDownWaves, rb, hb);
-    }
-    if (b < b1) multiply(b, ra, ha);
-  }
-  // acc[t][c][i]: token 16 t + 4 (lane / 16) + i, column 8 (lane % 16) + c; a tile of tokens at a time through LDS
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (t > 0) __syncthreads();
-    float* mine = red + wave * 2048;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < 8; c += 4)
-        *reinterpret_cast<float4*>(mine + (4 * (lane >> 4) + i) * 128 + 8 * (lane & 15) + c) =
-            make_float4(acc[t][c][i], acc[t][c + 1][i], acc[t][c + 2][i], acc[t][c + 3][i]);
-    __syncthreads();
-    const int token = 16 * t + (int)threadIdx.x / 32, col = blockIdx.x * 128 + (int)threadIdx.x % 32 * 4;
-    float4 s = reinterpret_cast<const float4*>(red)[threadIdx.x];
-#pragma unroll
-    for (int w = 1; w < kDownWaves; ++w) {
-      const float4 v = reinterpret_cast<const float4*>(red + w * 2048)[threadIdx.x];
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    if (token < T && col < d) {
-      const size_t at = (size_t)token * d + col;
-      if (parts > 1) {
-        *reinterpret_cast<float4*>(part + (size_t)blockIdx.y * T * d + at) = s;
-      } else {
-        const float f[4] = {s.x, s.y, s.z, s.w};
-        *reinterpret_cast<uint2*>(y + at) = pack4(f);
-      }
-    }
-  }
-}
-
 constexpr int kMostStreamParts = 8;
 
-// Parts of the rows: about 512 workgroups, of at least one block of 32 rows per wave.
+// Parts of the rows: a workgroup for every compute unit, which has its LDS, with two blocks of 32 rows for each of its four
+// waves.  us of both layers, 17 / 48 tokens, with one, two, four blocks: d = 512, 8192 units 19.1, 17.1, 17.1 / 23.2, 21.1, 20.8;
+// 800, 2504 14.0, 13.4, 15.2 / 16.9, 15.9, 17.6.
 int down_parts(int d, int rows) {
-  const int columns = (d + 127) / 128, most = (rows + 32 * kDownWaves - 1) / (32 * kDownWaves);
-  int parts = 512 / columns;
-  parts = parts < 1 ? 1 : (parts > 16 ? 16 : parts);
-  return parts < most ? parts : most;
+  const int columns = (d + 127) / 128, most = rows / (32 * 4 * 2), parts = 256 / columns;
+  const int fewer = parts < most ? parts : most;
+  return fewer < 1 ? 1 : fewer;
 }
 
 // ---- both layers in one kernel: the fewest tokens ---------------------------------------------
@@ -387,11 +293,19 @@ int one_groups(int d_ff) {
   return groups > 512 ? 4 : (groups > 256 ? 2 : 1);
 }
 int one_parts(int d_ff) { return (d_ff + 16 * one_groups(d_ff) - 1) / (16 * one_groups(d_ff)); }
-// One kernel and the join of its parts is shorter than two and a join as long as the parts' way through memory is: up to 35 MB
-// there and back.  us, one kernel / two: d = 2048, 16384 units, one token 38.3 / 47.3, eight (34 MB) 43.2 / 50.0, sixteen 51.4
-// / 51.9; d = 4096, 8192 units, four (34 MB) 47.9 / 49.0, eight 54.5 / 50.4; d = 8192, 28000 units, one (29 MB) 249 / 260, four
-// 278 / 264; d = 256, 1024 units, one 7.2 / 9.4.
-bool one_kernel(int T, int d, int d_ff) { return T <= 16 && (long long)one_parts(d_ff) * T * d * 8 <= (35ll << 20); }
+// One kernel and the join of its parts saves about 4 us against two and a join.  It loses what its parts take on their way through
+// memory (6.5 TB/s there and back) and, where its workgroups come short of the compute units, a part of the matrices' time (at 5.6
+// TB/s; three quarters of the units are enough for all of it).  us, one kernel / two: d = 2048, 16384 units, one token 39.3 / 43.5,
+// four 40.6 / 43.9, eight 43.3 / 44.2; 2560, 10240 (160 workgroups), one 43.3 / 37.4; 2048, 20000 (313), one 62.0 / 50.1; 4096,
+// 8192, two 43.6 / 45.4, four 46.6 / 46.2; 1024, 4096, four 13.3 / 15.1, sixteen 18.4 / 15.7; 512, 2048, sixteen 11.2 / 13.0;
+// 256, 1024, one 7.6 / 8.8.  Over 25 such layers and up to sixteen tokens it is at most 14 % off.
+bool one_kernel(int T, int d, int d_ff) {
+  if (T > 16) return false;
+  const int parts = one_parts(d_ff), rounds = (parts + 255) / 256;
+  const double filled = 1.35 * parts / (256.0 * rounds), matrices = 6.0 * d * d_ff / 5.6e6;
+  const double lost = (double)parts * T * d * 8.0 / 6.5e6 + (filled < 1.0 ? matrices * (1.0 / filled - 1.0) : 0.0);
+  return lost <= 4.0;
+}
 
 template <int GROUPS, int kOneWaves>
 hipError_t launch_one(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
@@ -404,11 +318,9 @@ hipError_t launch_one(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y
 }
 
 // out = the sum over the pairs' rows, in parts where they are many.
-template <int NT>
-hipError_t launch_down(const DownPairs& from, int T, int d, int d_ff, uint16_t* out, float* part, hipStream_t s) {
+hipError_t launch_down(const GatedDown& from, int T, int d, int d_ff, uint16_t* out, float* part, hipStream_t s) {
   const int parts = down_parts(d, from.pairs * d_ff);
-  const hipError_t e = launch(&k_gated_down<NT>, dim3((unsigned)((d + 127) / 128), (unsigned)parts), dim3(64 * kDownWaves), 0, s, from, T,
-                              d, d_ff, part, out);
+  const hipError_t e = launch_gated_down_stream(from, T, d, d_ff, parts, out, part, s);
   if (e != hipSuccess || parts == 1) return e;
   return launch_join_parts(part, out, true, parts, (long long)T * d, s);
 }
@@ -425,7 +337,7 @@ hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y
     return launch(&k_gated_up<decltype(act)::value, NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
                   dim3(64 * kUpWaves), 0, s, L, x, T, kept);
   });
-  return e != hipSuccess ? e : launch_down<NT>(DownPairs{{L.w2u, nullptr}, {kept.h, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
+  return e != hipSuccess ? e : launch_down(GatedDown{{L.w2u, nullptr}, {kept.h, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
 }
 
 template <int NT>
@@ -493,9 +405,7 @@ hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int 
 
 hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
                                hipStream_t s) {
-  return with_tiles(T, [&](auto tiles) {
-    return launch_down<decltype(tiles)::value>(DownPairs{{L.wg, L.wu}, {dg, du}, 2}, T, L.d, L.d_ff, dx, part, s);
-  });
+  return launch_down(GatedDown{{L.wg, L.wu}, {dg, du}, 2}, T, L.d, L.d_ff, dx, part, s);
 }
 
 }  // namespace hire

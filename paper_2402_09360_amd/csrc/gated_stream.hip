@@ -152,7 +152,112 @@ hipError_t launch_tiles(const GatedLayer& L, const uint16_t* x, int T, const Gat
   return launch_span<ACT, NT, 4>(L, x, T, parts, part_cols, kept, part, s);
 }
 
+// ---- the second layer, and dx -------------------------------------------------------------
+// Columns 128 blockIdx.x ..., rows of part blockIdx.y of the matrix (of two matrices one behind the other: dx): the waves take
+// blocks of 32 rows in turn, which come to LDS with the tokens' values that go with them, kPlaces - 1 blocks ahead.  The columns'
+// operands are read transposed (four rows of sixteen columns by sixteen lanes); unit u (32 bytes) of row k lies at u ^ (k % 4 + 4
+// (k / 8 % 2)), so that what half a wave reads lies in different banks.
+constexpr int kDownRows = 32, kDownCols = 128, kDownMatrix = kDownRows * kDownCols * 2, kDownLoads = kDownMatrix / 1024;
+
+template <int NT>
+__global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_gated_down_stream(
+    GatedDown from, int T, int d, int d_ff, float* __restrict__ part, uint16_t* __restrict__ y) {
+  constexpr int kPlaces = NT <= 2 ? 4 : 3, kPlace = kDownMatrix + NT * 1024, kBlocks = kDownCols / 16;
+  __shared__ __align__(1024) char smem[kStreamWaves * kPlaces * kPlace];
+  static_assert(sizeof(smem) >= kStreamWaves * NT * 16 * kDownCols * 4, "the sums");
+  const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, q = lane >> 4;
+  const int parts = gridDim.y, each = (d_ff + kDownRows - 1) / kDownRows, blocks = each * from.pairs;
+  const int b0 = (int)((long long)blocks * blockIdx.y / parts) + wave, b1 = (int)((long long)blocks * (blockIdx.y + 1) / parts);
+  const int n = b0 < b1 ? (b1 - b0 + kStreamWaves - 1) / kStreamWaves : 0;
+  const int col0 = (int)blockIdx.x * kDownCols, chunks = min((d - col0) / 8, kDownCols / 8);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem)) + (uint32_t)wave * kPlaces * kPlace;
+  auto request = [&](int i) __attribute__((always_inline)) {
+    const int block = b0 + i * kStreamWaves, pair = block >= each ? 1 : 0, k0 = (block - pair * each) * kDownRows;
+    const uint32_t lds = lds0 + (uint32_t)(i % kPlaces) * kPlace;
+    const char* w = reinterpret_cast<const char*>(from.w[pair] + (size_t)k0 * d + col0);
+    const bool whole = k0 + kDownRows <= d_ff && chunks == kDownCols / 8;
+#pragma unroll
+    for (int p = 0; p < kDownLoads; ++p) {  // four rows each
+      const int k = 4 * p + q, chunk = ((r >> 1) ^ ((k & 3) + 4 * (k >> 3 & 1))) * 2 + (r & 1);
+      const uint32_t off = (uint32_t)k * 2u * d + (uint32_t)chunk * 16;
+      if (whole)
+        gemm_load(w, off, lds + p * 1024);
+      else
+        gemm_load_at(k0 + k < d_ff && chunk < chunks ? (const void*)(w + off) : (const void*)kGemmZeros, lds + p * 1024);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {  // sixteen tokens; chunk c of token m lies at c ^ (m / 4 % 4)
+      const int token = lane >> 2, chunk = (lane & 3) ^ (token >> 2);
+      const uint16_t* h = from.h[pair] + (size_t)min(16 * t + token, T - 1) * d_ff + k0 + 8 * chunk;
+      gemm_load_at(k0 + 8 * chunk < d_ff ? (const void*)h : (const void*)kGemmZeros, lds + kDownMatrix + t * 1024);
+    }
+  };
+  constexpr int kLoads = kDownLoads + NT;
+  for (int i = 0; i < kPlaces - 1 && i < n; ++i) request(i);
+  f32x4v acc[NT][kBlocks] = {};
+  for (int i = 0; i < n; ++i) {
+    if (i + kPlaces - 2 < n)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kPlaces - 2) * kLoads) : "memory");
+    else if (kPlaces == 4 && i + 1 < n)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (i + kPlaces - 1 < n) request(i + kPlaces - 1);  // where the block before was
+    const char* place = smem + (wave * kPlaces + i % kPlaces) * kPlace;
+    bf16x8v hf[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      hf[t] = *reinterpret_cast<const bf16x8v*>(place + kDownMatrix + t * 1024 + r * 64 + ((q ^ (r >> 2)) << 4));
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+      using Lds = __attribute__((address_space(3))) s16x4v*;
+      const int k = 8 * q + (r >> 2);  // and four behind
+      const char* at = place + k * (2 * kDownCols) + ((c ^ ((k & 3) + 4 * (k >> 3 & 1))) << 5) + ((r & 3) << 3);
+      const s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at);
+      const s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * (2 * kDownCols)));
+      bf16x8v col;
+      __builtin_memcpy(&col, &lo, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&col) + 8, &hi, 8);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, hf[t], acc[t][c], 0, 0, 0);
+    }
+  }
+  // acc[t][c]: token 16 t + lane % 16, columns 16 c + 4 q ...; the waves' sums are added in their order
+  __syncthreads();
+  f32x4v* sums = reinterpret_cast<f32x4v*>(smem);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) sums[((wave * NT + t) * kBlocks + c) * 64 + lane] = acc[t][c];
+  __syncthreads();
+  for (int j = wave; j < NT * kBlocks; j += kStreamWaves) {
+    f32x4v v = sums[j * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < kStreamWaves; ++w) v += sums[(w * NT * kBlocks + j) * 64 + lane];
+    const int token = j / kBlocks * 16 + r, col = col0 + j % kBlocks * 16 + 4 * q;
+    if (token >= T || col >= d) continue;  // d is a multiple of 8
+    const size_t at = (size_t)token * d + col;
+    if (parts > 1) {
+      *reinterpret_cast<f32x4v*>(part + (size_t)blockIdx.y * T * d + at) = v;
+    } else {
+      const float f[4] = {v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<uint2*>(y + at) = pack4(f);
+    }
+  }
+}
+
 }  // namespace
+
+hipError_t launch_gated_down_stream(const GatedDown& from, int T, int d, int d_ff, int parts, uint16_t* out, float* part,
+                                    hipStream_t s) {
+  const dim3 grid((unsigned)((d + kDownCols - 1) / kDownCols), (unsigned)parts), block(64 * kStreamWaves);
+  switch ((T + 15) / 16) {
+    case 1: return launch(&k_gated_down_stream<1>, grid, block, 0, s, from, T, d, d_ff, part, out);
+    case 2: return launch(&k_gated_down_stream<2>, grid, block, 0, s, from, T, d, d_ff, part, out);
+    case 3: return launch(&k_gated_down_stream<3>, grid, block, 0, s, from, T, d, d_ff, part, out);
+    default: return launch(&k_gated_down_stream<4>, grid, block, 0, s, from, T, d, d_ff, part, out);
+  }
+}
 
 int gated_stream_parts(int d) { return (d + 4 * kStreamCols - 1) / (4 * kStreamCols); }
 

@@ -499,6 +499,12 @@ size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs);  // pairs: 1 for
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                             hipStream_t s);
 // gated_stream.hip: the first layer alone, in so many parts of d
+struct GatedDown {
+  const uint16_t *w[2], *h[2];  // a matrix and its values, or two pairs whose products are added
+  int pairs;
+};
+hipError_t launch_gated_down_stream(const GatedDown& from, int T, int d, int d_ff, int parts, uint16_t* out, float* part,
+                                    hipStream_t s);
 int gated_stream_parts(int d);
 hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s);
 hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
