@@ -64,6 +64,11 @@ __device__ __forceinline__ uint4 load_streaming(const uint4* p) {
   const u32x4 t = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
   return make_uint4(t.x, t.y, t.z, t.w);
 }
+// A store of what is not read again for a while: it leaves the caches to others.
+__device__ __forceinline__ void store_streaming(void* p, const uint4& v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+}
 
 // ---- order-preserving unsigned keys ----------------------------------------
 // a < b (as numbers, with -0 == +0 canonicalised to +0)  <=>  key(a) < key(b).

@@ -77,6 +77,58 @@ __global__ __launch_bounds__(256) void k_join_gated(const float* __restrict__ pa
   }
 }
 
+// dg = dh u a'(g), du = dh a(g) of eight units, rounded to bf16 for the products that follow.
+struct KeptEight {
+  uint4 g, u, low;
+};
+__device__ __forceinline__ KeptEight load_kept(const GatedKept& kept, size_t at) {
+  return KeptEight{*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
+                   *reinterpret_cast<const uint4*>(kept.low + at)};
+}
+template <int ACT>
+__device__ __forceinline__ void store_slopes(const KeptEight& k, const float (&dh)[8], uint16_t* dg, uint16_t* du) {
+  float gv[8], uv[8], dgv[8], duv[8];
+  unpack_kept(k.g, k.u, k.low, gv, uv);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float slope;
+    const float a = activation<ACT>(gv[e], &slope);
+    dgv[e] = dh[e] * uv[e] * slope;
+    duv[e] = dh[e] * a;
+  }
+  *reinterpret_cast<uint4*>(dg) = pack8(dgv);
+  *reinterpret_cast<uint4*>(du) = pack8(duv);
+}
+template <int ACT>
+__global__ __launch_bounds__(256) void k_join_slopes(const float* __restrict__ part, int parts, long long values, GatedKept kept,
+                                                     uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
+  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < values; i += (long long)gridDim.x * 2048) {
+    const KeptEight k = load_kept(kept, (size_t)i);
+    float dh[8];
+    join_eight(part + i, parts, (size_t)values, dh);
+    store_slopes<ACT>(k, dh, dg + i, du + i);
+  }
+}
+
+// Rows of up to three products in bf16.  STREAMING: past the caches, for the weights' gradients, whose writing is what the products
+// of few tokens are bound by (d = 2048, 16384 units, one token: 60 -> 36 us, a plain fill 34).
+template <bool STREAMING>
+struct StoreBf16 {
+  uint16_t* c[3];
+  template <int MB, int NB>
+  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int product,
+                                        int) const {
+    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
+      uint16_t* to = c[product] + (size_t)m * N + n;
+      if constexpr (STREAMING)
+        store_streaming(to, pack8(v[0]));
+      else
+        *reinterpret_cast<uint4*>(to) = pack8(v[0]);
+    });
+  }
+};
+hipError_t launch_gated_few_weights(const GemmArgs& g, const StoreBf16<true>& out, hipStream_t s);  // gated_few.hip: K up to 64
+
 // Calls f with the activation as a type.
 template <typename F>
 hipError_t with_activation(int act, F f) {

@@ -352,6 +352,52 @@ hipError_t launch_slopes(const GatedLayer& L, const uint16_t* dy, int T, const G
   });
 }
 
+// ---- the weights' gradients -------------------------------------------------------------------
+// out[f, c] = sum over the tokens of a[token, f] b[token, c], bound by writing it.  A workgroup has both operands of its 128 x 128
+// tile in LDS as a whole (32 tokens STEPS times), so little of it that four share a compute unit and fill each other's waits.  d =
+// 2048, 16384 units, one token, us of the three: 75 as tiles of the many tokens' kernel, 60 this way, 36 with streaming stores.
+template <int STEPS>
+__global__ __launch_bounds__(256) void k_gated_outer(GemmArgs g, StoreBf16<true> out) {
+  using Tile = GemmTile<128, 4, false, false>;
+  constexpr int kTiles = 2 * STEPS * Tile::kBytes, kRows = 4 * 32 * kRowFloats * 4;
+  __shared__ __align__(1024) char smem[kTiles > kRows ? kTiles : kRows];
+  const int tiles_m = (g.M + 127) / 128, tiles_n = (g.N + 127) / 128, tiles = tiles_m * tiles_n;
+  const int w = gemm_place((int)blockIdx.x, (int)gridDim.x), product = w / tiles, t = w % tiles;
+  const int m0 = t / tiles_n * 128, n0 = t % tiles_n * 128, wave = __builtin_amdgcn_readfirstlane(wave_id());
+  Tile ta, tb;
+  ta.init(m0, g.M, g.lda);
+  tb.init(n0, g.N, g.ldb);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
+  const char* a = static_cast<const char*>(g.a[product]) + 2 * (size_t)m0;
+  const char* b = static_cast<const char*>(g.b[product]) + 2 * (size_t)n0;
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int k = s * kGemmStep;
+    ta.request(a + (size_t)k * g.lda, nullptr, g.K - k, lds0 + 2 * s * Tile::kBytes, wave);
+    tb.request(b + (size_t)k * g.ldb, nullptr, g.K - k, lds0 + (2 * s + 1) * Tile::kBytes, wave);
+  }
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  const int wm = wave / 2 * 64, wn = wave % 2 * 64;
+  f32x16v acc[2][2] = {};
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8v fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = Tile::fragment(smem + 2 * s * Tile::kBytes, wm + 32 * i, ks);
+        fb[i] = Tile::fragment(smem + (2 * s + 1) * Tile::kBytes, wn + 32 * i, ks);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    }
+  lds_barrier();  // LDS is the epilogue's
+  out.store(acc, smem, m0 + wm, n0 + wn, g.M, g.N, product, 0);
+}
+
 // f with the number of tiles of sixteen tokens as a type.
 template <typename F>
 hipError_t with_tiles(int T, F f) {
@@ -379,9 +425,9 @@ hipError_t launch_few_by_width(const GatedLayer& L, const uint16_t* x, int T, ui
 
 size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs) {
   if (pairs == 1 && one_kernel(T, d, d_ff)) return (size_t)one_parts(d_ff) * T * d * sizeof(float);
-  const int parts = down_parts(d, pairs * d_ff), streams = pairs == 1 && few_streams(d, d_ff) ? gated_stream_parts(d) : 1;
+  const int parts = down_parts(d, pairs * d_ff), streams = few_streams(d, d_ff) ? gated_stream_parts(d) : 1;
   const size_t down = parts > 1 ? (size_t)parts * T * d * sizeof(float) : 0;
-  const size_t up = streams > 1 ? 2 * (size_t)streams * T * d_ff * sizeof(float) : 0;
+  const size_t up = streams > 1 ? (pairs == 1 ? 2 : 1) * (size_t)streams * T * d_ff * sizeof(float) : 0;  // g and u, or dh
   return down > up ? down : up;
 }
 
@@ -399,8 +445,17 @@ hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint1
 }
 
 hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
-                                   hipStream_t s) {
+                                   float* part, hipStream_t s) {
+  // streamed or not, us of this and dx: 17 / 64 tokens, d = 2560, 10240 units 45.7 / 57.8, 51.0 / 72.0, 8192, 2048 32.4 / 40.9, 38.3 /
+  // 64.6, 2048, 16384 50.3 / 64.2, 52.6 / 69.9; sixteen 48.6, 47.6; of 1024, 8192 23.9 / 35.5, 22.2 / 30.7
+  if (T > 16 && few_streams(L.d, L.d_ff) && (long long)L.d * L.d_ff >= 1 << 24)
+    return launch_gated_stream_slopes(L, dy, T, kept, dg, du, part, s);
   return with_tiles(T, [&](auto tiles) { return launch_slopes<decltype(tiles)::value>(L, dy, T, kept, dg, du, s); });
+}
+
+hipError_t launch_gated_few_weights(const GemmArgs& g, const StoreBf16<true>& out, hipStream_t s) {
+  const long long tiles = (long long)((g.M + 127) / 128) * ((g.N + 127) / 128) * g.products;
+  return launch(g.K <= kGemmStep ? &k_gated_outer<1> : &k_gated_outer<2>, dim3((unsigned)tiles), dim3(256), 0, s, g, out);
 }
 
 hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,

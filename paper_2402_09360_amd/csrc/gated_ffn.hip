@@ -4,17 +4,6 @@
 namespace hire {
 namespace {
 
-struct StoreBf16 {
-  uint16_t* c[3];
-  template <int MB, int NB>
-  __device__ __forceinline__ void store(const f32x16v (&acc)[MB][NB], char* smem, int m0, int n0, int M, int N, int product,
-                                        int) const {
-    for_rows<false>(acc, smem, m0, n0, M, N, NoFetch{}, [&](int m, int n, const float (&v)[1][8], int) {
-      *reinterpret_cast<uint4*>(c[product] + (size_t)m * N + n) = pack8(v[0]);
-    });
-  }
-};
-
 // h = a(g) u.
 template <int ACT>
 struct StoreGated {
@@ -26,28 +15,7 @@ struct StoreGated {
     });
   }
 };
-// dg = dh u a'(g), du = dh a(g) of eight units, rounded to bf16 for the products that follow.
-struct KeptEight {
-  uint4 g, u, low;
-};
-__device__ __forceinline__ KeptEight load_kept(const GatedKept& kept, size_t at) {
-  return KeptEight{*reinterpret_cast<const uint4*>(kept.g + at), *reinterpret_cast<const uint4*>(kept.u + at),
-                   *reinterpret_cast<const uint4*>(kept.low + at)};
-}
-template <int ACT>
-__device__ __forceinline__ void store_slopes(const KeptEight& k, const float (&dh)[8], uint16_t* dg, uint16_t* du) {
-  float gv[8], uv[8], dgv[8], duv[8];
-  unpack_kept(k.g, k.u, k.low, gv, uv);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float slope;
-    const float a = activation<ACT>(gv[e], &slope);
-    dgv[e] = dh[e] * uv[e] * slope;
-    duv[e] = dh[e] * a;
-  }
-  *reinterpret_cast<uint4*>(dg) = pack8(dgv);
-  *reinterpret_cast<uint4*>(du) = pack8(duv);
-}
+// The sums are dh.
 template <int ACT>
 struct StoreGateSlopes {
   GatedKept kept;
@@ -60,17 +28,6 @@ struct StoreGateSlopes {
     });
   }
 };
-template <int ACT>
-__global__ __launch_bounds__(256) void k_join_slopes(const float* __restrict__ part, int parts, long long values, GatedKept kept,
-                                                     uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
-  for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8; i < values; i += (long long)gridDim.x * 2048) {
-    const KeptEight k = load_kept(kept, (size_t)i);
-    float dh[8];
-    join_eight(part + i, parts, (size_t)values, dh);
-    store_slopes<ACT>(k, dh, dg + i, du + i);
-  }
-}
-
 constexpr int kMostSplits = 32;
 int k_steps(int k) { return (k + kGemmStep - 1) / kGemmStep; }
 ProductShape up_shape(int T, int d, int d_ff) { return product_shape(T, 2 * d_ff, k_steps(d), 1, kMostSplits); }
@@ -84,8 +41,8 @@ ProductShape units_shape(int T, int d, int d_ff, int segments) {
 size_t split_bytes(const ProductShape& shape, size_t values) { return shape.splits > 1 ? shape.splits * values * sizeof(float) : 0; }
 
 // Up to three products of one shape with bf16 results, split over k where their tiles are few.
-template <bool AK, bool BK>
-hipError_t launch_split_products(GemmArgs g, const ProductShape& shape, const StoreBf16& out, float* part, hipStream_t s) {
+template <bool AK, bool BK, bool STREAMING>
+hipError_t launch_split_products(GemmArgs g, const ProductShape& shape, const StoreBf16<STREAMING>& out, float* part, hipStream_t s) {
   g.splits = shape.splits;
   if (g.splits == 1) return launch_product<AK, BK, false, false>(g, shape.tile, out, s);
   const hipError_t e = launch_product<AK, BK, false, false>(g, shape.tile, StorePart<false>{part, g.splits}, s);
@@ -104,12 +61,12 @@ size_t gated_forward_part_bytes(int T, int d, int d_ff) {
 }
 
 size_t gated_backward_part_bytes(int T, int d, int d_ff) {
+  const bool few = T <= kGatedFewTokens;
   size_t weights = 0;
-  for (int products = 1; products <= 3; ++products) {
+  for (int products = 1; products <= 3 && !few; ++products) {
     const size_t bytes = split_bytes(weights_shape(T, d, d_ff, products), products * (size_t)d_ff * d);
     if (bytes > weights) weights = bytes;
   }
-  const bool few = T <= kGatedFewTokens;
   const size_t slopes = few ? 0 : split_bytes(slopes_shape(T, d, d_ff), (size_t)T * d_ff);
   const size_t dx = few ? gated_few_part_bytes(T, d, d_ff, 2) : split_bytes(units_shape(T, d, d_ff, 2), (size_t)T * d);
   const size_t most = weights > slopes ? weights : slopes;
@@ -140,7 +97,7 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
   down.a[0] = kept.h, down.b[0] = L.w2u;
   down.M = T, down.N = L.d, down.K = L.d_ff, down.lda = 2u * L.d_ff, down.ldb = 2u * L.d;
   down.segments = down.products = 1;
-  return launch_split_products<true, false>(down, units_shape(T, L.d, L.d_ff, 1), StoreBf16{{y, nullptr, nullptr}}, part, s);
+  return launch_split_products<true, false>(down, units_shape(T, L.d, L.d_ff, 1), StoreBf16<false>{{y, nullptr, nullptr}}, part, s);
 }
 
 hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
@@ -149,7 +106,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   hipError_t e = hipSuccess;
   const bool few = T <= kGatedFewTokens;
   if (few && (dx || dwg || dwu)) {
-    e = launch_gated_few_slopes(L, dy, T, kept, dg, du, s);
+    e = launch_gated_few_slopes(L, dy, T, kept, dg, du, part, s);
   } else if (dx || dwg || dwu) {
     GemmArgs a{};
     a.a[0] = dy, a.b[0] = L.w2u;
@@ -169,7 +126,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   }
   if (e != hipSuccess) return e;
   GemmArgs w{};
-  StoreBf16 out{};
+  StoreBf16<true> out{};
   auto add = [&](const uint16_t* a, const uint16_t* b, uint16_t* c) {
     if (c) w.a[w.products] = a, w.b[w.products] = b, out.c[w.products++] = c;
   };
@@ -178,8 +135,9 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
   add(kept.h, dy, dw2u);
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
-    w.segments = 1;
-    e = launch_split_products<false, false>(w, weights_shape(T, L.d, L.d_ff, w.products), out, part, s);
+    w.segments = w.splits = 1;
+    e = few ? launch_gated_few_weights(w, out, s)
+            : launch_split_products<false, false>(w, weights_shape(T, L.d, L.d_ff, w.products), out, part, s);
     if (e != hipSuccess) return e;
   }
   if (dx && few) return launch_gated_few_dx(L, T, dg, du, dx, part, s);
@@ -188,7 +146,7 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
     a.a[0] = dg, a.a[1] = du, a.b[0] = L.wg, a.b[1] = L.wu;
     a.M = T, a.N = L.d, a.K = L.d_ff, a.lda = 2u * L.d_ff, a.ldb = 2u * L.d;
     a.segments = 2, a.products = 1;
-    e = launch_split_products<true, false>(a, units_shape(T, L.d, L.d_ff, 2), StoreBf16{{dx, nullptr, nullptr}}, part, s);
+    e = launch_split_products<true, false>(a, units_shape(T, L.d, L.d_ff, 2), StoreBf16<false>{{dx, nullptr, nullptr}}, part, s);
   }
   return e;
 }

@@ -1,9 +1,7 @@
-// The dense gated FFN's first layer for 17 to 64 tokens: bound by reading both matrices once.
-//   A wave keeps 512 columns of the tokens in registers for as long as it lives and works on sixteen units after the other.  Their
-// rows come to LDS by asynchronous loads of runs of 512 bytes: a place holds 256 columns of sixteen rows of one matrix, three
-// places are on their way while one is multiplied (96 KB for the four waves of a compute unit), and as every wave has its own, no
-// barrier is among them.  SPAN waves share units whose rows have up to 512 SPAN columns and add their sums; longer rows are split
-// into parts.
+// The dense gated FFN for few tokens with large layers: bound by reading the matrices once.  Rows come to LDS by asynchronous loads
+// of runs of 512 bytes (256 in the second layer), three places ahead (about 96 KB on their way for the four waves of a compute
+// unit); every wave has its own places, so that no barrier is among them.  d = 2048, 16384 units, 48 tokens, us against rows that
+// come to registers a step or two ahead: first layer 37 -> 30, second 21 -> 18, dh 30 -> 22.
 #include "gated.h"
 
 namespace hire {
@@ -12,11 +10,17 @@ namespace {
 constexpr int kStreamWaves = 4, kStreamCols = 512, kStreamHalf = kStreamCols / 2, kStreamPlaces = 4;
 constexpr int kStreamPlace = 16 * kStreamHalf * 2, kStreamLoads = kStreamPlace / 1024;
 
-// part null: h and what is kept; else the sums of columns blockIdx.y, in StorePart<true>'s order.
-template <int ACT, int NT, int SPAN>
+// ---- the first layer, and dh ------------------------------------------------------------------
+// A wave keeps 512 columns of the tokens in registers for as long as it lives and works on sixteen units after the other.  A place
+// holds 256 columns of sixteen rows of one matrix.  SPAN waves share units whose rows have up to 512 SPAN columns and add their
+// sums; longer rows are split into parts.
+//   part null: h and what is kept; else the sums of columns blockIdx.y, in StorePart's order.
+// SLOPES: x is dy and the one matrix is the second layer's, 32 units at a time; dg and du instead of h.
+template <bool SLOPES, int ACT, int NT, int SPAN>
 __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_gated_stream(
-    GatedLayer L, const uint16_t* __restrict__ x, int T, int part_cols, GatedKept kept, float* __restrict__ part) {
-  constexpr int kGroups = kStreamWaves / SPAN, kSteps = kStreamHalf / 32;
+    GatedLayer L, const uint16_t* __restrict__ x, int T, int part_cols, GatedKept kept, uint16_t* __restrict__ dg,
+    uint16_t* __restrict__ du, float* __restrict__ part) {
+  constexpr int kGroups = kStreamWaves / SPAN, kUnits = SLOPES ? 32 : 16, kSteps = kStreamHalf / 32;
   __shared__ __align__(1024) char smem[kStreamWaves * kStreamPlaces * kStreamPlace];
   __shared__ f32x4v join[SPAN > 1 ? kStreamWaves * 2 * NT * 64 : 1];
   const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, q = lane >> 4;
@@ -35,16 +39,16 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
     }
   }
 
-  const int sixteens = (L.d_ff + 15) / 16, batches = (sixteens + kGroups - 1) / kGroups;
+  const int batches = (L.d_ff + kUnits * kGroups - 1) / (kUnits * kGroups);
   const int n = (batches - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;  // at least one
-  auto unit_of = [&](int i) { return (((int)blockIdx.x + i * (int)gridDim.x) * kGroups + wave / SPAN) * 16; };
+  auto unit_of = [&](int i) { return (((int)blockIdx.x + i * (int)gridDim.x) * kGroups + wave / SPAN) * kUnits; };
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem)) + (uint32_t)wave * kStreamPlaces * kStreamPlace;
   const uint32_t ld = 2u * L.d;
-  // Place p of units i: the gate's first and second 256 columns, then the other matrix's.  A load is two rows; chunk c of row r lies
-  // at c ^ r.
+  // Place p of units i: the gate's first and second 256 columns, then the other matrix's (SLOPES: the other units').  A load is two
+  // rows; chunk c of row r lies at c ^ r.
   auto request = [&](int i, int p) __attribute__((always_inline)) {
-    const int unit0 = min(unit_of(i), L.d_ff - 1), last = L.d_ff - 1 - unit0, ahead = p % 2 * (kStreamHalf / 8);
-    const char* base = reinterpret_cast<const char*>(p < 2 ? L.wg : L.wu) + (size_t)unit0 * ld + 2 * (size_t)col0 + 16 * ahead;
+    const int unit0 = min(unit_of(i) + (SLOPES ? p / 2 * 16 : 0), L.d_ff - 1), last = L.d_ff - 1 - unit0, ahead = p % 2 * (kStreamHalf / 8);
+    const char* base = reinterpret_cast<const char*>(SLOPES ? L.w2u : (p < 2 ? L.wg : L.wu)) + (size_t)unit0 * ld + 2 * (size_t)col0 + 16 * ahead;
     const uint32_t lds = lds0 + (uint32_t)p * kStreamPlace;
 #pragma unroll
     for (int k = 0; k < kStreamLoads; ++k) {
@@ -90,30 +94,64 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
     for (int m = 0; m < 2; ++m)
 #pragma unroll
       for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(acc[m][t]));
-    // token 16 t + lane % 16, units 4 q ... of the sixteen
-    auto store = [&](int t, const f32x4v& g, const f32x4v& u) __attribute__((always_inline)) {
-      const int token = 16 * t + r, unit = unit_of(i) + 4 * q;
-      if (token >= T || unit >= L.d_ff) return;  // d_ff is a multiple of 8
-      const size_t at = (size_t)token * L.d_ff + unit, units = (size_t)T * L.d_ff;
-      if (part) {
-        float* to = part + 2 * blockIdx.y * units + at;
-        *reinterpret_cast<f32x4v*>(to) = g;
-        *reinterpret_cast<f32x4v*>(to + units) = u;
-        return;
-      }
-      float h[4], slope;
+    // token 16 t + lane % 16, units 4 q ... of the sixteen (SLOPES: of both)
+    auto store = [&](int t, const f32x4v (&v)[2]) __attribute__((always_inline)) {
+      const int token = 16 * t + r;
+      const size_t units = (size_t)T * L.d_ff;
+      if constexpr (SLOPES) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = activation<ACT>(g[e], &slope) * u[e];
-      *reinterpret_cast<uint2*>(kept.h + at) = pack4(h);
-      if (kept.g) {
-        *reinterpret_cast<uint2*>(kept.g + at) = make_uint2(upper_pair(g[0], g[1]), upper_pair(g[2], g[3]));
-        *reinterpret_cast<uint2*>(kept.u + at) = make_uint2(upper_pair(u[0], u[1]), upper_pair(u[2], u[3]));
-        *reinterpret_cast<uint2*>(kept.low + at) = make_uint2(lower_pair(g[0], u[0], g[1], u[1]), lower_pair(g[2], u[2], g[3], u[3]));
+        for (int m = 0; m < 2; ++m) {
+          const int unit = unit_of(i) + 16 * m + 4 * q;
+          if (token >= T || unit >= L.d_ff) continue;  // d_ff is a multiple of 8
+          const size_t at = (size_t)token * L.d_ff + unit;
+          if (part) {
+            *reinterpret_cast<f32x4v*>(part + blockIdx.y * units + at) = v[m];
+            continue;
+          }
+          const uint2 gd = *reinterpret_cast<const uint2*>(kept.g + at), ud = *reinterpret_cast<const uint2*>(kept.u + at);
+          const uint2 ld = *reinterpret_cast<const uint2*>(kept.low + at);
+          const uint32_t g[2] = {gd.x, gd.y}, u[2] = {ud.x, ud.y}, low[2] = {ld.x, ld.y};
+          float dgv[4], duv[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int shift = e % 2 * 16;
+            const uint32_t l = low[e / 2] >> shift;
+            const float gv = __uint_as_float((g[e / 2] >> shift) << 16 | (l & 0xFFu) << 8);
+            const float uv = __uint_as_float((u[e / 2] >> shift) << 16 | (l & 0xFF00u));
+            float slope;
+            const float a = activation<ACT>(gv, &slope);
+            dgv[e] = v[m][e] * uv * slope;
+            duv[e] = v[m][e] * a;
+          }
+          *reinterpret_cast<uint2*>(dg + at) = pack4(dgv);
+          *reinterpret_cast<uint2*>(du + at) = pack4(duv);
+        }
+      } else {
+        const int unit = unit_of(i) + 4 * q;
+        if (token >= T || unit >= L.d_ff) return;
+        const size_t at = (size_t)token * L.d_ff + unit;
+        const f32x4v g = v[0], u = v[1];
+        if (part) {
+          float* to = part + 2 * blockIdx.y * units + at;
+          *reinterpret_cast<f32x4v*>(to) = g;
+          *reinterpret_cast<f32x4v*>(to + units) = u;
+          return;
+        }
+        float h[4], slope;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = activation<ACT>(g[e], &slope) * u[e];
+        *reinterpret_cast<uint2*>(kept.h + at) = pack4(h);
+        if (kept.g) {
+          *reinterpret_cast<uint2*>(kept.g + at) = make_uint2(upper_pair(g[0], g[1]), upper_pair(g[2], g[3]));
+          *reinterpret_cast<uint2*>(kept.u + at) = make_uint2(upper_pair(u[0], u[1]), upper_pair(u[2], u[3]));
+          *reinterpret_cast<uint2*>(kept.low + at) =
+              make_uint2(lower_pair(g[0], u[0], g[1], u[1]), lower_pair(g[2], u[2], g[3], u[3]));
+        }
       }
     };
     if constexpr (SPAN == 1) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) store(t, acc[0][t], acc[1][t]);
+      for (int t = 0; t < NT; ++t) store(t, {acc[0][t], acc[1][t]});
     } else {
       if (i > 0) lds_barrier();  // the sums before are read
 #pragma unroll
@@ -123,33 +161,54 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
       lds_barrier();
       for (int t = in_span; t < NT; t += SPAN) {
         const f32x4v* first = join + ((wave - in_span) * 2 * NT + t) * 64 + lane;
-        f32x4v g = first[0], u = first[NT * 64];
+        f32x4v v[2] = {first[0], first[NT * 64]};
 #pragma unroll
-        for (int w = 1; w < SPAN; ++w) g += first[w * 2 * NT * 64], u += first[(w * 2 + 1) * NT * 64];
-        store(t, g, u);
+        for (int w = 1; w < SPAN; ++w) v[0] += first[w * 2 * NT * 64], v[1] += first[(w * 2 + 1) * NT * 64];
+        store(t, v);
       }
     }
   }
 }
 
-template <int ACT, int NT, int SPAN>
-hipError_t launch_span(const GatedLayer& L, const uint16_t* x, int T, int parts, int part_cols, const GatedKept& kept, float* part,
-                       hipStream_t s) {
-  constexpr int kUnits = 16 * (kStreamWaves / SPAN);
-  const int batches = (L.d_ff + kUnits - 1) / kUnits, each = 256 / parts;
-  const hipError_t e = launch(&k_gated_stream<ACT, NT, SPAN>, dim3((unsigned)(batches < each ? batches : each), (unsigned)parts),
-                              dim3(64 * kStreamWaves), 0, s, L, x, T, part_cols, kept, parts > 1 ? part : nullptr);
+struct FirstLayer {
+  GatedLayer L;
+  const uint16_t* x;
+  int T;
+  GatedKept kept;
+  uint16_t *dg, *du;  // SLOPES
+  float* part;
+};
+template <bool SLOPES, int ACT, int NT, int SPAN>
+hipError_t launch_span(const FirstLayer& f, int parts, int part_cols, hipStream_t s) {
+  constexpr int kUnits = (SLOPES ? 32 : 16) * (kStreamWaves / SPAN);
+  const int batches = (f.L.d_ff + kUnits - 1) / kUnits, each = 256 / parts;
+  const hipError_t e = launch(&k_gated_stream<SLOPES, ACT, NT, SPAN>, dim3((unsigned)(batches < each ? batches : each), (unsigned)parts),
+                              dim3(64 * kStreamWaves), 0, s, f.L, f.x, f.T, part_cols, f.kept, f.dg, f.du,
+                              parts > 1 ? f.part : nullptr);
   if (e != hipSuccess || parts == 1) return e;
-  const long long units = (long long)T * L.d_ff;
-  return launch(&k_join_gated<ACT>, dim3(join_blocks(units / 8)), dim3(256), 0, s, part, parts, units, kept);
+  const long long units = (long long)f.T * f.L.d_ff;
+  const dim3 grid(join_blocks(units / 8)), block(256);
+  if constexpr (SLOPES) return launch(&k_join_slopes<ACT>, grid, block, 0, s, f.part, parts, units, f.kept, f.dg, f.du);
+  else return launch(&k_join_gated<ACT>, grid, block, 0, s, f.part, parts, units, f.kept);
 }
-
-template <int ACT, int NT>
-hipError_t launch_tiles(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s) {
-  const int parts = gated_stream_parts(L.d), part_cols = (L.d / 8 + parts - 1) / parts * 8;
-  if (part_cols <= kStreamCols) return launch_span<ACT, NT, 1>(L, x, T, parts, part_cols, kept, part, s);
-  if (part_cols <= 2 * kStreamCols) return launch_span<ACT, NT, 2>(L, x, T, parts, part_cols, kept, part, s);
-  return launch_span<ACT, NT, 4>(L, x, T, parts, part_cols, kept, part, s);
+template <bool SLOPES, int ACT, int NT>
+hipError_t launch_tiles(const FirstLayer& f, hipStream_t s) {
+  const int d = f.L.d, parts = gated_stream_parts(d), part_cols = (d / 8 + parts - 1) / parts * 8;
+  if (part_cols <= kStreamCols) return launch_span<SLOPES, ACT, NT, 1>(f, parts, part_cols, s);
+  if (part_cols <= 2 * kStreamCols) return launch_span<SLOPES, ACT, NT, 2>(f, parts, part_cols, s);
+  return launch_span<SLOPES, ACT, NT, 4>(f, parts, part_cols, s);
+}
+template <bool SLOPES>
+hipError_t launch_first_layer(const FirstLayer& f, hipStream_t s) {
+  return with_activation(f.L.act, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    switch ((f.T + 15) / 16) {
+      case 1: return launch_tiles<SLOPES, ACT, 1>(f, s);
+      case 2: return launch_tiles<SLOPES, ACT, 2>(f, s);
+      case 3: return launch_tiles<SLOPES, ACT, 3>(f, s);
+      default: return launch_tiles<SLOPES, ACT, 4>(f, s);
+    }
+  });
 }
 
 // ---- the second layer, and dx -------------------------------------------------------------
@@ -262,15 +321,11 @@ hipError_t launch_gated_down_stream(const GatedDown& from, int T, int d, int d_f
 int gated_stream_parts(int d) { return (d + 4 * kStreamCols - 1) / (4 * kStreamCols); }
 
 hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s) {
-  return with_activation(L.act, [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
-    switch ((T + 15) / 16) {
-      case 1: return launch_tiles<ACT, 1>(L, x, T, kept, part, s);
-      case 2: return launch_tiles<ACT, 2>(L, x, T, kept, part, s);
-      case 3: return launch_tiles<ACT, 3>(L, x, T, kept, part, s);
-      default: return launch_tiles<ACT, 4>(L, x, T, kept, part, s);
-    }
-  });
+  return launch_first_layer<false>(FirstLayer{L, x, T, kept, nullptr, nullptr, part}, s);
+}
+hipError_t launch_gated_stream_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+                                      float* part, hipStream_t s) {
+  return launch_first_layer<true>(FirstLayer{L, dy, T, kept, dg, du, part}, s);
 }
 
 }  // namespace hire

@@ -498,17 +498,19 @@ constexpr int kGatedFewTokens = 64;
 size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs);  // pairs: 1 forward, 2 dx
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                             hipStream_t s);
-// gated_stream.hip: the first layer alone, in so many parts of d
+// gated_stream.hip: the first layer, or dg and du, in so many parts of d; and the second layer, or dx, in `parts` of the rows
+int gated_stream_parts(int d);
+hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s);
+hipError_t launch_gated_stream_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+                                      float* part, hipStream_t s);
 struct GatedDown {
   const uint16_t *w[2], *h[2];  // a matrix and its values, or two pairs whose products are added
   int pairs;
 };
 hipError_t launch_gated_down_stream(const GatedDown& from, int T, int d, int d_ff, int parts, uint16_t* out, float* part,
                                     hipStream_t s);
-int gated_stream_parts(int d);
-hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, float* part, hipStream_t s);
 hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
-                                   hipStream_t s);
+                                   float* part, hipStream_t s);
 hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
                                hipStream_t s);
 

@@ -134,7 +134,8 @@ def test_products_in_parts(hire, T, d, F, act):
 
 @pytest.mark.parametrize("T,d,F,act", [
     (17, 1024, 8200, "silu"), (40, 2056, 4104, "gelu"), (64, 3000, 2808, "silu"), (33, 5000, 1688, "gelu"),
-    (48, 16384, 520, "silu"), (12, 8192, 4104, "gelu"), (16, 2048, 16384, "silu"), (31, 1032, 8136, "gelu")])
+    (48, 16384, 520, "silu"), (12, 8192, 4104, "gelu"), (16, 2048, 16384, "silu"), (31, 1032, 8136, "gelu"),
+    (40, 2056, 8200, "gelu"), (64, 5000, 3400, "silu"), (17, 1032, 16400, "silu")])
 def test_few_tokens_of_large_layers(hire, T, d, F, act):
     print(f"T={T} d={d} F={F} {act}", flush=True)
     data = inputs(T + d, T, d, F)
