@@ -548,14 +548,13 @@ def _tensor(t, dtype, shape, where):
 
 def _room(workspace, where):
     """Address and bytes of a workspace on the current device."""
-    if not workspace.is_contiguous() or workspace.get_device() != _current_device():
+    if workspace.get_device() != _current_device() or not workspace.is_contiguous():
         raise HireError(EINVAL, f"{where}: a contiguous workspace on the current device wanted, got one on {workspace.device}")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
-def _on_device(device, what, where):
-    if device.index != _current_device():
-        raise HireError(EINVAL, f"{where}: {what} on the current device wanted, got {device}")
+def _elsewhere(what, where):
+    return HireError(EINVAL, f"{where}: {what} on the current device wanted")
 
 
 ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2
@@ -571,7 +570,7 @@ class GatedLayer:
                 raise HireError(EINVAL, "GatedLayer: contiguous bf16 [d_ff, d_model] matrices of one device")
         if act not in _ACTS:
             raise HireError(EINVAL, f"GatedLayer: act is one of {sorted(_ACTS)}")
-        self.wg, self.wu, self.w2u, self.act, self.device = wg, wu, w2u, act, wg.device
+        self.wg, self.wu, self.w2u, self.act, self.device_index = wg, wu, w2u, act, wg.get_device()
         self.d_ff, self.d_model = wg.shape
         self.c = _GatedLayer(self.d_model, self.d_ff, wg.data_ptr(), wu.data_ptr(), w2u.data_ptr(), _ACTS[act])
         self.ref = C.byref(self.c)
@@ -611,7 +610,8 @@ def hire_gated_ffn_step(layer: GatedLayer, x: torch.Tensor, out: GatedOutputs, w
                         stream=None) -> None:
     """Enqueue the dense gated FFN of x bf16 [T, d_model]."""
     where, bf16, T = "hire_gated_ffn_step", torch.bfloat16, x.shape[0]
-    _on_device(layer.device, "the layer", where)
+    if layer.device_index != _current_device():
+        raise _elsewhere("a layer", where)
     tokens = (T, layer.d_model)
     saved = None if out.saved is None else _tensor(out.saved, torch.uint8, (hire_gated_ffn_saved_bytes(layer, T),), where)
     _check(_lib.hire_gated_ffn_step(layer.ref, _tensor(x, bf16, tokens, where), T, _tensor(out.y, bf16, tokens, where), saved,
@@ -622,7 +622,8 @@ def hire_gated_ffn_backward(layer: GatedLayer, x: torch.Tensor, out: GatedOutput
                             grads: GatedGradients, workspace: torch.Tensor, stream=None) -> None:
     """Enqueue the gradients for dy bf16 [T, d_model]; `out` as the forward call with train=True left it."""
     where, bf16, T = "hire_gated_ffn_backward", torch.bfloat16, x.shape[0]
-    _on_device(layer.device, "the layer", where)
+    if layer.device_index != _current_device():
+        raise _elsewhere("a layer", where)
     tokens, weights = (T, layer.d_model), (layer.d_ff, layer.d_model)
     if out.saved is None:
         raise HireError(EINVAL, f"{where}: outputs made with train=True")
@@ -657,7 +658,8 @@ class Mxfp4:
                    torch.empty((rows, cols // 32), dtype=torch.uint8, device=device))
 
     def _addresses(self, where):
-        _on_device(self.codes.device, "a packed matrix", where)
+        if self.codes.get_device() != _current_device():
+            raise _elsewhere("a packed matrix", where)
         return self.codes.data_ptr(), self.scales.data_ptr()
 
 
@@ -737,7 +739,7 @@ class Drafts:
 
         p, p_idx = rows(target_prob, target_idx, n + 1, 0)
         q, q_idx = rows(draft_prob, draft_idx, n, 1)
-        self.B, self.n, self.vocab, self.device = B, n, vocab, tokens.device
+        self.B, self.n, self.vocab, self.device, self.device_index = B, n, vocab, tokens.device, tokens.get_device()
         self.tensors = (tokens, target_prob, target_idx, draft_prob, draft_idx, accept_u, sample_u, lengths)
         self.c = _Drafts(B, n, vocab, None if lengths is None else _tensor(lengths, i32, (B,), where),
                          _tensor(tokens, i32, (B, n), where) or None, p, p_idx, k[0] or 0, q, q_idx, k[1] or 0,
@@ -760,7 +762,8 @@ def hire_verify_draft_workspace_bytes(drafts: Drafts) -> int:
 def hire_verify_draft(drafts: Drafts, out: DraftOutputs, workspace: torch.Tensor, stream=None) -> None:
     """Enqueue the verification: the accepted tokens and the one that follows, and how many were accepted."""
     where = "hire_verify_draft"
-    _on_device(drafts.device, "the drafts", where)
+    if drafts.device_index != _current_device():
+        raise _elsewhere("drafts", where)
     _check(_lib.hire_verify_draft(drafts.ref, _tensor(out.tokens, torch.int32, (drafts.B, drafts.n + 1), where),
                                   _tensor(out.accepted, torch.int32, (drafts.B,), where), *_room(workspace, where),
                                   _stream(stream)), where)
