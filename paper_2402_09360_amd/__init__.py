@@ -1,4 +1,4 @@
-"""MI355X-native HiRE decode-step hot path (HiRE-FFN, HiRE-Softmax, top-k select).
+"""MI355X-native HiRE decode-step hot path (HiRE-FFN, HiRE-Softmax, top-k select) and the dense operators next to it.
 
 Sub-modules are imported on demand so that the input generators can be used
 without the GPU library:

@@ -1,6 +1,6 @@
-// The dense gated FFN for up to 64 tokens, forward, and backward but for the weights' gradients: bound by reading the three
-// matrices once (6 d d_ff bytes).  Tokens are the
-// small side of 16 x 16 x 32 matrix instructions, whose other operand comes straight from memory into registers.
+// The dense gated FFN for up to 64 tokens, forward and backward: bound by reading the three matrices once (6 d d_ff bytes), and by
+// writing their gradients.  Tokens are the small side of 16 x 16 x 32 matrix instructions, whose other operand comes straight from
+// memory into registers; large layers are streamed through LDS instead (gated_stream.hip).
 #include "gated.h"
 
 namespace hire {
