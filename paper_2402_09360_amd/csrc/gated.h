@@ -23,6 +23,13 @@ __device__ __forceinline__ float activation(float g, float* slope) {
   }
 }
 
+// The same where few values of a kernel go through it.
+__device__ __forceinline__ float activation_of(int act, float g, float* slope) {
+  if (act == kActRelu) return activation<kActRelu>(g, slope);
+  if (act == kActSilu) return activation<kActSilu>(g, slope);
+  return activation<kActGelu>(g, slope);
+}
+
 // What the forward call keeps for the backward one: planes of 16 bits per unit and token.  h is rounded to bf16 as the second
 // product reads it.  g and u keep 24 bits of their fp32 (15 of the significand), the upper 16 in planes of their own and the
 // lower 8 of both in a third (GatedKept): rounded to bf16 they would add their error to that of dg and du, 0.0030 relative to

@@ -113,7 +113,7 @@ __device__ __forceinline__ void keep_gated(const GatedKept& kept, size_t at, flo
 
 constexpr int kUpWaves = 4;
 
-template <int ACT, int NT, int RU>
+template <int NT, int RU>
 __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const uint16_t* __restrict__ x, int T, GatedKept kept) {
   __shared__ float red[kUpWaves * 2 * NT * 256];
   const int unit0 = blockIdx.x * 16 * RU;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const 
         if (token >= T || f >= L.d_ff) return;
         const size_t at = (size_t)token * L.d_ff + f;
         float slope;
-        const __bf16 h = (__bf16)(activation<ACT>(v[0], &slope) * v[1]);
+        const __bf16 h = (__bf16)(activation_of(L.act, v[0], &slope) * v[1]);
         __builtin_memcpy(kept.h + at, &h, 2);
         if (kept.g) keep_gated(kept, at, v[0], v[1]);
       });
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const 
 }
 
 // The backward pass's first product: dh of the units, and from it and what was kept dg and du.
-template <int ACT, int NT, int RU>
+template <int NT, int RU>
 __global__ __launch_bounds__(64 * kUpWaves) void k_gated_slopes(GatedLayer L, const uint16_t* __restrict__ dy, int T, GatedKept kept,
                                                                 uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
   __shared__ float red[kUpWaves * NT * 256];
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_slopes(GatedLayer L, co
         const float gv = __uint_as_float((uint32_t)kept.g[at] << 16 | (low & 0xFFu) << 8);
         const float uv = __uint_as_float((uint32_t)kept.u[at] << 16 | (low & 0xFF00u));
         float slope;
-        const float a = activation<ACT>(gv, &slope);
+        const float a = activation_of(L.act, gv, &slope);
         const __bf16 dgv = (__bf16)(dh[0] * uv * slope), duv = (__bf16)(dh[0] * a);
         __builtin_memcpy(dg + at, &dgv, 2);
         __builtin_memcpy(du + at, &duv, 2);
@@ -333,10 +333,9 @@ bool few_streams(int d, int d_ff) { return d >= 1024 && (long long)d * d_ff >= 1
 
 template <int NT, int RU>
 hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part, hipStream_t s) {
-  const hipError_t e = few_streams(L.d, L.d_ff) ? launch_gated_stream(L, x, T, kept, part, s) : with_activation(L.act, [&](auto act) {
-    return launch(&k_gated_up<decltype(act)::value, NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
-                  dim3(64 * kUpWaves), 0, s, L, x, T, kept);
-  });
+  const hipError_t e = few_streams(L.d, L.d_ff) ? launch_gated_stream(L, x, T, kept, part, s)
+                                               : launch(&k_gated_up<NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
+                                                        dim3(64 * kUpWaves), 0, s, L, x, T, kept);
   return e != hipSuccess ? e : launch_down(GatedDown{{L.w2u, nullptr}, {kept.h, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
 }
 
@@ -344,12 +343,9 @@ template <int NT>
 hipError_t launch_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
                          hipStream_t s) {
   const int groups = (L.d_ff + 15) / 16;
-  return with_activation(L.act, [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
-    if (groups >= 2 * 256)
-      return launch(&k_gated_slopes<ACT, NT, 2>, dim3((unsigned)((groups + 1) / 2)), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
-    return launch(&k_gated_slopes<ACT, NT, 1>, dim3((unsigned)groups), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
-  });
+  if (groups >= 2 * 256)
+    return launch(&k_gated_slopes<NT, 2>, dim3((unsigned)((groups + 1) / 2)), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
+  return launch(&k_gated_slopes<NT, 1>, dim3((unsigned)groups), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
 }
 
 // ---- the weights' gradients -------------------------------------------------------------------

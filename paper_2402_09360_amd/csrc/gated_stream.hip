@@ -16,7 +16,7 @@ constexpr int kStreamPlace = 16 * kStreamHalf * 2, kStreamLoads = kStreamPlace /
 // sums; longer rows are split into parts.
 //   part null: h and what is kept; else the sums of columns blockIdx.y, in StorePart's order.
 // SLOPES: x is dy and the one matrix is the second layer's, 32 units at a time; dg and du instead of h.
-template <bool SLOPES, int ACT, int NT, int SPAN>
+template <bool SLOPES, int NT, int SPAN>
 __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_gated_stream(
     GatedLayer L, const uint16_t* __restrict__ x, int T, int part_cols, GatedKept kept, uint16_t* __restrict__ dg,
     uint16_t* __restrict__ du, float* __restrict__ part) {
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
             const float gv = __uint_as_float((g[e / 2] >> shift) << 16 | (l & 0xFFu) << 8);
             const float uv = __uint_as_float((u[e / 2] >> shift) << 16 | (l & 0xFF00u));
             float slope;
-            const float a = activation<ACT>(gv, &slope);
+            const float a = activation_of(L.act, gv, &slope);
             dgv[e] = v[m][e] * uv * slope;
             duv[e] = v[m][e] * a;
           }
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
         }
         float h[4], slope;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = activation<ACT>(g[e], &slope) * u[e];
+        for (int e = 0; e < 4; ++e) h[e] = activation_of(L.act, g[e], &slope) * u[e];
         *reinterpret_cast<uint2*>(kept.h + at) = pack4(h);
         if (kept.g) {
           *reinterpret_cast<uint2*>(kept.g + at) = make_uint2(upper_pair(g[0], g[1]), upper_pair(g[2], g[3]));
@@ -178,37 +178,37 @@ struct FirstLayer {
   uint16_t *dg, *du;  // SLOPES
   float* part;
 };
-template <bool SLOPES, int ACT, int NT, int SPAN>
+template <bool SLOPES, int NT, int SPAN>
 hipError_t launch_span(const FirstLayer& f, int parts, int part_cols, hipStream_t s) {
   constexpr int kUnits = (SLOPES ? 32 : 16) * (kStreamWaves / SPAN);
   const int batches = (f.L.d_ff + kUnits - 1) / kUnits, each = 256 / parts;
-  const hipError_t e = launch(&k_gated_stream<SLOPES, ACT, NT, SPAN>, dim3((unsigned)(batches < each ? batches : each), (unsigned)parts),
+  const hipError_t e = launch(&k_gated_stream<SLOPES, NT, SPAN>, dim3((unsigned)(batches < each ? batches : each), (unsigned)parts),
                               dim3(64 * kStreamWaves), 0, s, f.L, f.x, f.T, part_cols, f.kept, f.dg, f.du,
                               parts > 1 ? f.part : nullptr);
   if (e != hipSuccess || parts == 1) return e;
   const long long units = (long long)f.T * f.L.d_ff;
   const dim3 grid(join_blocks(units / 8)), block(256);
-  if constexpr (SLOPES) return launch(&k_join_slopes<ACT>, grid, block, 0, s, f.part, parts, units, f.kept, f.dg, f.du);
-  else return launch(&k_join_gated<ACT>, grid, block, 0, s, f.part, parts, units, f.kept);
+  return with_activation(f.L.act, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if constexpr (SLOPES) return launch(&k_join_slopes<ACT>, grid, block, 0, s, f.part, parts, units, f.kept, f.dg, f.du);
+    else return launch(&k_join_gated<ACT>, grid, block, 0, s, f.part, parts, units, f.kept);
+  });
 }
-template <bool SLOPES, int ACT, int NT>
+template <bool SLOPES, int NT>
 hipError_t launch_tiles(const FirstLayer& f, hipStream_t s) {
   const int d = f.L.d, parts = gated_stream_parts(d), part_cols = (d / 8 + parts - 1) / parts * 8;
-  if (part_cols <= kStreamCols) return launch_span<SLOPES, ACT, NT, 1>(f, parts, part_cols, s);
-  if (part_cols <= 2 * kStreamCols) return launch_span<SLOPES, ACT, NT, 2>(f, parts, part_cols, s);
-  return launch_span<SLOPES, ACT, NT, 4>(f, parts, part_cols, s);
+  if (part_cols <= kStreamCols) return launch_span<SLOPES, NT, 1>(f, parts, part_cols, s);
+  if (part_cols <= 2 * kStreamCols) return launch_span<SLOPES, NT, 2>(f, parts, part_cols, s);
+  return launch_span<SLOPES, NT, 4>(f, parts, part_cols, s);
 }
 template <bool SLOPES>
 hipError_t launch_first_layer(const FirstLayer& f, hipStream_t s) {
-  return with_activation(f.L.act, [&](auto act) {
-    constexpr int ACT = decltype(act)::value;
-    switch ((f.T + 15) / 16) {
-      case 1: return launch_tiles<SLOPES, ACT, 1>(f, s);
-      case 2: return launch_tiles<SLOPES, ACT, 2>(f, s);
-      case 3: return launch_tiles<SLOPES, ACT, 3>(f, s);
-      default: return launch_tiles<SLOPES, ACT, 4>(f, s);
-    }
-  });
+  switch ((f.T + 15) / 16) {
+    case 1: return launch_tiles<SLOPES, 1>(f, s);
+    case 2: return launch_tiles<SLOPES, 2>(f, s);
+    case 3: return launch_tiles<SLOPES, 3>(f, s);
+    default: return launch_tiles<SLOPES, 4>(f, s);
+  }
 }
 
 // ---- the second layer, and dx -------------------------------------------------------------
