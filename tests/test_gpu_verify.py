@@ -209,6 +209,27 @@ def test_lists_with_repeats_and_padding(hire, dense_target):
         same(hire, c)
 
 
+@pytest.mark.parametrize("target,draft", [("dense", "dense"), ("dense", "list"), ("list", "list"), ("list", "dense")])
+def test_rows_that_start_anywhere(hire, target, draft):
+    """Distributions at addresses that are multiples of four bytes and of nothing more."""
+    c = draw(77, 5, 3, 2048, target, draft, 100, ragged=False)
+    want = expected(c, exact=False)
+
+    def moved(name):
+        if c.get(name) is None:
+            return None
+        t = torch.from_numpy(np.ascontiguousarray(c[name]))
+        buffer = torch.empty(t.numel() + 8, dtype=t.dtype, device="cuda")
+        buffer[1:1 + t.numel()] = t.cuda().flatten()
+        return buffer[1:1 + t.numel()].view(t.shape)
+
+    drafts = hire.Drafts(moved("tokens"), c["vocab"], moved("target"), moved("accept_u"), moved("sample_u"),
+                         target_idx=moved("target_idx"), draft_prob=moved("draft"), draft_idx=moved("draft_idx"))
+    out = hire.DraftOutputs(drafts)
+    hire.hire_verify_draft(drafts, out, hire.alloc_workspace(hire.hire_verify_draft_workspace_bytes(drafts)))
+    assert np.array_equal(out.tokens.cpu().numpy(), want[0]) and np.array_equal(out.accepted.cpu().numpy(), want[1])
+
+
 def test_repeats_are_equal(hire):
     for target, draft in (("dense", "dense"), ("list", "list")):
         c = draw(5, 7, 4, 9000, target, draft, 300)
