@@ -326,9 +326,9 @@ hipError_t launch_down(const GatedDown& from, int T, int d, int d_ff, uint16_t* 
 }
 
 // The first layer's rows streamed past the tokens (gated_stream.hip): where they keep every compute unit at it for a while.  us of
-// both layers without / with it, 17 / 48 tokens: d = 2048, 16384 units 52.3, 51.2 / 59.7, 54.8; 2560, 10240 66.5, 49.8 / 80.5,
-// 57.1; 8192, 8192 93.9, 89.2 / 122, 98; 1024, 8192 24.7, 24.6 / 29.5, 28.0; not 1024, 4096 18.3, 19.4 / 22.5, 24.3 or 512, 8192 20.6,
-// 22.6 / 23.4, 26.6.
+// both layers without / with it, 17 / 48 tokens: d = 2048, 16384 units 49.7, 48.6 / 58.9, 53.7; 2560, 10240 57.9, 41.3 / 71.5,
+// 47.9; 8192, 8192 98, 88 / 121, 93; 1024, 8192 24.1, 23.3 / 28.9, 27.3; not 1024, 4096 16.7, 17.4 / 20.7, 22.5 or 512, 8192 17.4,
+// 18.8 / 21.5, 23.8.
 bool few_streams(int d, int d_ff) { return d >= 1024 && (long long)d * d_ff >= 1 << 23 && gated_stream_parts(d) <= kMostStreamParts; }
 
 template <int NT, int RU>

@@ -602,12 +602,12 @@ size_t mx_padded_bytes(int T, int rows, int cols) {
 // other tile and number of parts was timed for 16 such sizes: at most 9 % better.
 ProductShape mx_shape(int T, int rows, int cols) { return product_shape(T, rows, (cols + 127) / 128, 1, 32); }
 // Rows streamed past the tokens (mxfp4_stream.hip): matrices that keep every compute unit at it for a while.  us without / with it:
-//   bf16, two / sixteen tokens: 4096 rows of 4096 columns 6.1, 5.5 / 8.3, 7.4, of 1024 3.7, 4.9 / 4.3, 6.9 (no), 8192 of 2048 5.3,
-// 5.5 / 6.8, 7.2, 256000 of 2048 66.8, 61.2 / 72.4, 58.6, 12000 of 8192 23.8, 18.2 / 32.4, 20.1; rows in parts (more than 4096
-// columns) pay later: 4096 of 8192 9.6, 10.0 / 13.8, 12.2.  20: 12000 of 8192 31.7, 25.9, 65536 of 2048 23.5, 27.5 (no).
-//   packed, one / sixteen: 8192 of 2048 5.0, 4.8 / 6.0, 5.3, of 1024 4.0, 4.4 / 4.6, 5.1 (no), 16384 of 16384 45.7, 30.0 / 49.9,
-// 31.8; 20: 8192 of 1024 6.6, 5.8, 4096 of 1024 5.0, 5.6 (no); 48 / 64: 8192 of 4096 15.8, 11.2 / 18.3, 13.2, 20000 of 8192 31.7,
-// 28.4 / 34.1, 31.6, but 65536 of 2048 20.9, 23.0 / 22.2, 25.7 (no: tiles).
+//   bf16, two / sixteen tokens: 4096 rows of 4096 columns 6.0, 5.6 / 8.4, 7.5, of 1024 3.7, 5.0 / 4.4, 7.0 (no), 8192 of 2048 5.4,
+// 5.6 / 6.9, 7.4, 256000 of 2048 69.1, 56.7 / 76.2, 62.2, 12000 of 8192 24.1, 18.7 / 33.2, 21.1; rows in parts (more than 4096
+// columns) pay later: 4096 of 8192 9.9, 10.4 / 14.3, 12.7.  20: 12000 of 8192 32.6, 26.1, 65536 of 2048 24.6, 27.7 (no).
+//   packed, one / sixteen: 8192 of 2048 4.9, 4.8 / 5.9, 5.3, of 1024 3.9, 4.4 / 4.6, 5.1 (no), 16384 of 16384 48.0, 33.6 / 52.1,
+// 35.5; 20: 8192 of 1024 6.5, 5.8, 4096 of 1024 5.0, 5.6 (no); 48 / 64: 8192 of 4096 15.9, 11.4 / 18.1, 13.6, 20000 of 8192 34.1,
+// 30.6 / 36.4, 33.8, but 65536 of 2048 21.8, 24.3 / 22.9, 26.6 (no: tiles).
 bool mx_streams(int T, int rows, int cols, bool packed) {
   if (cols % 512 != 0 || cols < 1024 || T > (packed ? kMxFewTokens : 32) || (T == 1 && !packed)) return false;
   const long long values = (long long)rows * cols;

@@ -3,8 +3,8 @@
 // of these columns after the other.  The codes come to LDS by asynchronous loads of whole runs of 512 bytes, three sixteens ahead
 // (26 KB on their way for each of the four waves of a compute unit), without a barrier: every wave has its own places.  SPAN waves
 // share rows of up to 1024 SPAN columns and add their sums; longer rows are split into parts.  Against tokens that come from the L2
-// or LDS and codes that come to registers one step ahead, in pieces of 64 bytes: 60000 rows of 8192 columns, two bf16 tokens 71 ->
-// 56 us, sixteen 83 -> 59 (4.5 TB/s), sixteen packed ones 73 -> 57.
+// or LDS and codes that come to registers one step ahead, in pieces of 64 bytes: 60000 rows of 8192 columns, two bf16 tokens 74 ->
+// 55 us (4.8 TB/s), sixteen 88 -> 61, sixteen packed ones 78 -> 60.
 #include "mxfp4.h"
 
 #include "dense_epilogue.h"
