@@ -531,8 +531,12 @@ struct MxProduct {
 };
 size_t mx_workspace_bytes(int T, int rows, int cols);
 hipError_t launch_mx_product(const MxProduct& p, hipStream_t s);
-// mxfp4_stream.hip: many rows of whole 512 columns, their scale bytes 16-byte aligned, with a few tokens; parts: of the columns.
-int mx_stream_parts(int cols);
+// mxfp4_stream.hip: many rows of whole 512 columns, their scale bytes 16-byte aligned, with a few tokens.
+struct MxStreamShape {
+  int cols, parts;  // columns of a wave; parts of a row's columns
+  bool full;        // at least seven eighths of the waves' columns are there
+};
+MxStreamShape mx_stream_shape(bool packed, int T, int rows, int cols);
 hipError_t launch_mx_stream(const MxProduct& p, hipStream_t s);
 
 // ---- verify.hip: drafted tokens against the target's probabilities ----------------

@@ -602,18 +602,26 @@ size_t mx_padded_bytes(int T, int rows, int cols) {
 // other tile and number of parts was timed for 16 such sizes: at most 9 % better.
 ProductShape mx_shape(int T, int rows, int cols) { return product_shape(T, rows, (cols + 127) / 128, 1, 32); }
 // Rows streamed past the tokens (mxfp4_stream.hip): matrices that keep every compute unit at it for a while.  us without / with it:
-//   bf16, two / sixteen tokens: 4096 rows of 4096 columns 6.0, 5.6 / 8.4, 7.5, of 1024 3.7, 5.0 / 4.4, 7.0 (no), 8192 of 2048 5.4,
-// 5.6 / 6.9, 7.4, 256000 of 2048 69.1, 56.7 / 76.2, 62.2, 12000 of 8192 24.1, 18.7 / 33.2, 21.1; rows in parts (more than 4096
-// columns) pay later: 4096 of 8192 9.9, 10.4 / 14.3, 12.7.  20: 12000 of 8192 32.6, 26.1, 65536 of 2048 24.6, 27.7 (no).
-//   packed, one / sixteen: 8192 of 2048 4.9, 4.8 / 5.9, 5.3, of 1024 3.9, 4.4 / 4.6, 5.1 (no), 16384 of 16384 48.0, 33.6 / 52.1,
-// 35.5; 20: 8192 of 1024 6.5, 5.8, 4096 of 1024 5.0, 5.6 (no); 48 / 64: 8192 of 4096 15.9, 11.4 / 18.1, 13.6, 20000 of 8192 34.1,
-// 30.6 / 36.4, 33.8, but 65536 of 2048 21.8, 24.3 / 22.9, 26.6 (no: tiles).
+//   bf16, two / sixteen tokens: 4096 rows of 4096 columns 6.1, 5.6 / 8.4, 7.6, of 1024 3.7, 5.0 / 4.4, 5.1 (no), 8192 of 2048 5.4,
+// 5.9 / 6.9, 6.5, 256000 of 2048 69.5, 58.2 / 76.6, 64.3, 12000 of 8192 23.6, 19.0 / 32.6, 21.4; parts pay later: 4096 of 8192 9.8,
+// 10.1 / 14.1, 12.6.  20 / 48: 1000 of 2048 7.1, 5.9 / 9.5, 8.8, 20000 of 8192 50.1, 34.6 / 72.0, 42.2, 60000 of 8192 93.9, 77.3 /
+// 105, 97; 4096 of 1024 5.7, 6.1 / 7.8, 9.1 (no), 65536 of 2048 24.5, 25.9 / 26.5, 31.2 (no), 2048 of 4096, 48 11.1, 11.4 (no).
+//   packed, one / sixteen: 1000 of 2048 3.5, 3.2 / 4.3, 3.6, 8192 of 1024 4.0, 3.9 / 4.6, 4.1, 256000 of 2048 65.1, 56.1 / 67.5, 61.0,
+// 16384 of 16384 48.8, 33.4 / 52.4, 34.8; 20 / 64: 1000 of 2048 6.6, 4.0 / 9.2, 6.5, 8192 of 2048 9.0, 5.7 / 14.5, 8.6, 20000 of 8192
+// 42.5, 26.3 / 35.9, 33.3, but 64 on 65536 of 2048 22.9, 26.6 (no: tiles).
+//   Over 140 drawn sizes 0.93 of the time without it as a geometric mean, 0.49 to 1.1.
 bool mx_streams(int T, int rows, int cols, bool packed) {
-  if (cols % 512 != 0 || cols < 1024 || T > (packed ? kMxFewTokens : 32) || (T == 1 && !packed)) return false;
+  if (cols % 512 != 0 || cols < 1024 || T > kMxFewTokens || (T == 1 && !packed)) return false;
   const long long values = (long long)rows * cols;
-  if (T <= 16) return values >= 1 << 24 && (mx_stream_parts(cols) == 1 || T > 8 || values > 1 << 26);
-  if (!packed) return cols >= 4096 && values >= 1 << 26;
-  return values >= 1 << 23 && (T <= 32 || rows < 16384 || cols >= 4096);
+  const MxStreamShape shape = mx_stream_shape(packed, T, rows, cols);
+  if (!shape.full || shape.parts > 64 || values < 3 << 19) return false;
+  const bool long_rows = cols >= 4096;
+  if (T <= 16) {
+    if (shape.parts > 1 && T <= 8 && values <= 1 << 26) return false;
+    return packed || values >= 1 << 24 || (T > 8 && cols >= 2048);
+  }
+  if (packed) return T <= 32 || rows < 16384 || long_rows;
+  return (rows < 32768 || long_rows) && (cols >= 2048 || values >= 1 << 23) && (T <= 32 || shape.parts == 1 || values >= 1 << 24);
 }
 size_t mx_parts_bytes(int splits, int T, int rows) { return splits > 1 ? (size_t)splits * T * rows * sizeof(float) : 0; }
 }  // namespace
@@ -624,9 +632,13 @@ size_t mx_workspace_bytes(int T, int rows, int cols) {
       mx_tiles(T, rows) ? mx_padded_bytes(T, rows, cols) + mx_parts_bytes(mx_shape(T, rows, cols).splits, T, rows) : 0;
   if (T > kMxFewTokens) return tiles;
   // a call's alignment and tokens may allow the rows to be streamed or not
-  const int splits = few_splits(T, rows, cols), streams = mx_streams(T, rows, cols, true) || mx_streams(T, rows, cols, false)
-                                                              ? mx_stream_parts(cols) : 1;
-  const size_t parts = mx_parts_bytes(splits > streams ? splits : streams, T, rows);
+  int splits = few_splits(T, rows, cols);
+  for (const bool packed : {false, true})
+    if (mx_streams(T, rows, cols, packed)) {
+      const int streams = mx_stream_shape(packed, T, rows, cols).parts;
+      if (streams > splits) splits = streams;
+    }
+  const size_t parts = mx_parts_bytes(splits, T, rows);
   return parts > tiles ? parts : tiles;
 }
 

@@ -182,8 +182,9 @@ def test_products_in_parts(hire, T, rows, cols, dtype):
     product_case(hire, T, rows, cols, True, dtype)
 
 
-@pytest.mark.parametrize("rows,cols", [(16397, 1024), (10923, 1536), (8205, 2048), (5001, 4096), (8200, 8192), (13500, 5120)])
-@pytest.mark.parametrize("T,packed", [(2, False), (9, False), (16, False), (31, False), (1, True), (16, True), (32, True), (47, True),
+@pytest.mark.parametrize("rows,cols", [(16397, 1024), (10923, 1536), (8205, 2048), (5001, 4096), (8200, 8192), (13500, 5120),
+                                       (901, 2048), (1999, 7168)])
+@pytest.mark.parametrize("T,packed", [(2, False), (9, False), (16, False), (31, False), (33, False), (64, False), (1, True), (16, True), (32, True), (47, True),
                                       (64, True)])
 def test_streamed_rows(hire, T, packed, rows, cols):
     print(f"T={T} {rows}x{cols} packed={packed}", flush=True)
