@@ -553,6 +553,12 @@ def _room(workspace, where):
     return workspace.data_ptr(), workspace.nbytes
 
 
+def _allocating(stream):
+    """Results are allocated on the stream that writes them: what the current stream's allocator hands out may still be in
+    use by work queued there, which another stream does not wait for."""
+    return torch.cuda.stream(stream)   # None: the current one
+
+
 def _elsewhere(what, where):
     return HireError(EINVAL, f"{where}: {what} on the current device wanted")
 
@@ -664,22 +670,24 @@ class Mxfp4:
 
 
 def hire_pack_mxfp4(w: torch.Tensor, out: Mxfp4 | None = None, stream=None) -> Mxfp4:
-    """w bf16 [rows, cols] in microscaled 4-bit floating point; out: where to write it."""
+    """w bf16 [rows, cols] in microscaled 4-bit floating point; out: where to write it (else new tensors of the stream)."""
     where = "hire_pack_mxfp4"
     if w.dim() != 2:
         raise HireError(EINVAL, f"{where}: a matrix")
     if out is None:
-        out = Mxfp4.empty(w.shape[0], w.shape[1], w.device)
+        with _allocating(stream):
+            out = Mxfp4.empty(w.shape[0], w.shape[1], w.device)
     at = _tensor(w, torch.bfloat16, (out.rows, out.cols), where)
     _check(_lib.hire_pack_mxfp4(at, out.rows, out.cols, *out._addresses(where), _stream(stream)), where)
     return out
 
 
 def hire_unpack_mxfp4(w: Mxfp4, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """The values a packed matrix stands for, bf16 [rows, cols]."""
+    """The values a packed matrix stands for, bf16 [rows, cols]; out as for hire_pack_mxfp4."""
     where = "hire_unpack_mxfp4"
     if out is None:
-        out = torch.empty((w.rows, w.cols), dtype=torch.bfloat16, device=w.codes.device)
+        with _allocating(stream):
+            out = torch.empty((w.rows, w.cols), dtype=torch.bfloat16, device=w.codes.device)
     at = _tensor(out, torch.bfloat16, (w.rows, w.cols), where)
     _check(_lib.hire_unpack_mxfp4(*w._addresses(where), w.rows, w.cols, at, _stream(stream)), where)
     return out
