@@ -185,6 +185,12 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _allocating(stream):
+    """Results are allocated on the stream that writes them: what the current stream's allocator hands out may still be in
+    use by work queued there, which another stream does not wait for."""
+    return torch.cuda.stream(stream)   # None: the current one
+
+
 _FIVE_NONE = (None,) * 5
 
 
@@ -279,14 +285,16 @@ def hire_pack_int4(w_bf16: torch.Tensor, stream=None):
     nbytes = hire_pack_int4_bytes(rows, cols)
     if nbytes == 0:
         raise HireError(EINVAL, "hire_pack_int4_bytes")
-    q4 = torch.empty(nbytes, dtype=torch.uint8, device=w_bf16.device)
-    scale = torch.empty(rows, dtype=torch.float32, device=w_bf16.device)
+    with _allocating(stream):
+        q4 = torch.empty(nbytes, dtype=torch.uint8, device=w_bf16.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=w_bf16.device)
     _check(_lib.hire_pack_int4(_ptr(w_bf16), rows, cols, _ptr(q4), _ptr(scale), _stream(stream)), "hire_pack_int4")
     return q4, scale
 
 
 def hire_unpack_int4(q4: torch.Tensor, rows: int, cols: int, stream=None) -> torch.Tensor:
-    codes = torch.empty((rows, cols), dtype=torch.int8, device=q4.device)
+    with _allocating(stream):
+        codes = torch.empty((rows, cols), dtype=torch.int8, device=q4.device)
     _check(_lib.hire_unpack_int4(_ptr(q4), rows, cols, _ptr(codes), _stream(stream)), "hire_unpack_int4")
     return codes
 
@@ -525,6 +533,9 @@ def topk_select(scores: torch.Tensor, k: int, relu: bool = False, rank_order: bo
     """Indices (int32 [B,k]) and values (fp32 [B,k]) of the k largest entries of each row of scores fp32 [B,N].
     workspace: one from alloc_workspace(hire_topk_workspace_bytes(...)) to reuse over calls of the same shape (long
     rows then select through its histograms from the second call on); a fresh one is made otherwise."""
+    if stream is not None:
+        with _allocating(stream):
+            return topk_select(scores, k, relu, rank_order, want_values, workspace=workspace)
     assert scores.is_cuda and scores.dtype == torch.float32 and scores.is_contiguous() and scores.dim() == 2
     B, N = scores.shape
     flags = (RELU if relu else 0) | (ORDER_RANK if rank_order else 0)
@@ -551,12 +562,6 @@ def _room(workspace, where):
     if workspace.get_device() != _current_device() or not workspace.is_contiguous():
         raise HireError(EINVAL, f"{where}: a contiguous workspace on the current device wanted, got one on {workspace.device}")
     return workspace.data_ptr(), workspace.nbytes
-
-
-def _allocating(stream):
-    """Results are allocated on the stream that writes them: what the current stream's allocator hands out may still be in
-    use by work queued there, which another stream does not wait for."""
-    return torch.cuda.stream(stream)   # None: the current one
 
 
 def _elsewhere(what, where):
