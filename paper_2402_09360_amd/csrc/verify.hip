@@ -341,17 +341,18 @@ __global__ __launch_bounds__(kWave* kShortWaves) void k_verify_short(DraftArgs a
     for (int e = 0; e < EACH; ++e)
       if ((unsigned)q.token[e] < (unsigned)a.vocab) table.insert(q.token[e], e * kWave + lane);
     __builtin_amdgcn_wave_barrier();
-    float* probs = reinterpret_cast<float*>(keys);  // by place, once the places are found
+    // Probabilities by place, in the keys' words once the places are found: as bits of the same type, for a store through another
+    // one may be moved in front of the reads of the keys, and the barriers here are the wave's only
     int found[EACH];
 #pragma unroll
     for (int e = 0; e < EACH; ++e) found[e] = whole[e] > 0.0 ? table.find(p.token[e]) : 0x7FFFFFFF;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) probs[e * kWave + lane] = q.prob[e];
+    for (int e = 0; e < EACH; ++e) keys[e * kWave + lane] = __float_as_int(q.prob[e]);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
-      if (found[e] != 0x7FFFFFFF) rest[e] = fmax(whole[e] - (double)probs[found[e]], 0.0);
+      if (found[e] != 0x7FFFFFFF) rest[e] = fmax(whole[e] - (double)__int_as_float(keys[found[e]]), 0.0);
   }
   // running sums in the order of the places: blocks of 64 one after the other
   auto pick = [&](const double (&w)[EACH], int* next) {
