@@ -344,7 +344,7 @@ int hire_mxfp4_product_bf16(const void* x, int T, const void* w_codes, const voi
  * (u_i from [0, 1), q the draft's distribution, p the target's).  Behind the a accepted ones one more token follows: with
  * r(v) = max(p_a(v) - q_a(v), 0) if token a was refused, r = p_a if none was left (or if no r(v) is positive), it is
  * the first v with  sum_{w <= v} r(w) > s sum_w r(w),  s from [0, 1); -1 if p_a has no positive value.  Differences
- * and sums are fp64.
+ * and sums are fp64; where s is within 2^-45 of the border between two tokens, either may be the one.
  * A distribution is a dense row of `vocab` probabilities, where "first" counts tokens, or a list of k (token, probability)
  * pairs as hire_softmax_step leaves it, 0 elsewhere, where "first" counts places in the target's list.  Of entries that
  * name one token the first counts; entries whose token is not in [0, vocab) do not.  A drafted token outside [0, vocab)
@@ -358,7 +358,7 @@ typedef struct hire_drafts {
   int n;                      /* most drafted tokens of a sequence, 0 .. HIRE_MAX_DRAFT */
   int vocab;                  /* 1 .. HIRE_MAX_DRAFT_VOCAB */
   const int32_t* lengths;     /* optional [B]: drafted tokens of each sequence (clamped to 0 .. n); NULL: n */
-  const int32_t* tokens;      /* [B, n]; places behind a sequence's length are not read */
+  const int32_t* tokens;      /* [B, n]; what stands behind a sequence's length does not count, here and below */
   const float* target_prob;   /* fp32 [B, n + 1, vocab], or [B, n + 1, target_k] */
   const int32_t* target_idx;  /* lists: int32 [B, n + 1, target_k]; NULL: dense */
   int target_k;               /* 1 .. HIRE_MAX_RANK_ORDER_K, lists only */
