@@ -282,9 +282,9 @@ typedef struct hire_gated_layer {
 } hire_gated_layer;
 
 /* x, y: bf16 [T, d_model], 1 <= T <= HIRE_GATED_MAX_TOKENS; y is rounded once from fp32 sums over h, and h is rounded
- * to bf16 between the two layers.  saved: hire_gated_ffn_saved_bytes(L, T) bytes, 256-byte aligned, that receive what
- * hire_gated_ffn_backward reads (opaque: h in bf16, g and u in 24 bits), or NULL where no backward pass follows; y does not
- * depend on it.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on invalid arguments, never 0 on valid ones),
+ * to bf16 between the two layers (up to 16 tokens: to two bf16 terms, 16 bits of its significand).  saved:
+ * hire_gated_ffn_saved_bytes(L, T) bytes, 256-byte aligned, that receive what hire_gated_ffn_backward reads (opaque: h in
+ * bf16, g and u in 24 bits), or NULL where no backward pass follows; y does not depend on it.  workspace: hire_gated_ffn_workspace_bytes(L, T) bytes (0 on invalid arguments, never 0 on valid ones),
  * 256-byte aligned; no initialisation needed, and hire_workspace_init does no harm.  Outputs overlap neither inputs nor
  * each other, here and below.  HIRE_EUNSUPPORTED: T or a width beyond the limits above. */
 size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T);
@@ -296,7 +296,8 @@ int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y
  *   dh = <v_j, dy_b>;  dg = dh u a'(g);  du = dh a(g)   (a'(0) = 0 for HIRE_ACT_RELU)
  *   dw2u_j = sum_b h_bj dy_b;  dwg_j = sum_b dg_bj x_b;  dwu_j = sum_b du_bj x_b;  dx_b = sum_j dg_bj wg_j + du_bj wu_j
  * dx bf16 [T, d_model]; dwg, dwu, dw2u bf16 [d_ff, d_model]: each is written whole (nothing is added to what was there),
- * and each may be NULL, at least one not.  Sums are fp32, rounded once; dg and du are rounded to bf16 in between.
+ * and each may be NULL, at least one not.  Sums are fp32, rounded once; in between dg and du are rounded to
+ * bf16, as h was (up to 16 tokens: each to two bf16 terms; g and u, of which they are made, are held in 24 bits).
  * Results are the same from call to call.  Alignment, workspace (hire_gated_ffn_backward_workspace_bytes) and errors as
  * for the forward call. */
 size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T);

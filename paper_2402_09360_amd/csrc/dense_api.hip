@@ -81,6 +81,10 @@ GatedKept kept_planes(const hire_gated_layer* L, int T, void* saved) {
   const size_t plane = hidden_bytes(L, T);
   return GatedKept{bf16_at(saved, 0), bf16_at(saved, plane), bf16_at(saved, 2 * plane), bf16_at(saved, 3 * plane)};
 }
+bool keeps_rest(int T) { return T <= kGatedRestTokens; }
+// Planes at the front of a workspace: h and its rest; dg, du, their rests and that of h.
+size_t forward_planes(const hire_gated_layer* L, int T) { return (keeps_rest(T) ? 2 : 1) * hidden_bytes(L, T); }
+size_t backward_planes(const hire_gated_layer* L, int T) { return (keeps_rest(T) ? 5 : 2) * hidden_bytes(L, T); }
 
 }  // namespace
 
@@ -88,7 +92,7 @@ extern "C" {
 
 size_t hire_gated_ffn_workspace_bytes(const hire_gated_layer* L, int T) {
   if (check_gated(L, T) != HIRE_OK) return 0;
-  return hidden_bytes(L, T) + align_up(gated_forward_part_bytes(T, L->d_model, L->d_ff));
+  return forward_planes(L, T) + align_up(gated_forward_part_bytes(T, L->d_model, L->d_ff));
 }
 
 size_t hire_gated_ffn_saved_bytes(const hire_gated_layer* L, int T) {
@@ -101,15 +105,16 @@ int hire_gated_ffn_step(const hire_gated_layer* L, const void* x, int T, void* y
   if (!gated_weights(L) || !given(x, 16) || !given(y, 16) || !optional(saved, 256) || !given(workspace, 256))
     return HIRE_EINVAL;
   if (workspace_bytes < hire_gated_ffn_workspace_bytes(L, T)) return HIRE_ENOSPC;
-  const GatedKept kept = saved ? kept_planes(L, T, saved) : GatedKept{bf16_at(workspace, 0), nullptr, nullptr, nullptr};
-  float* part = reinterpret_cast<float*>(bf16_at(workspace, hidden_bytes(L, T)));
+  GatedKept kept = saved ? kept_planes(L, T, saved) : GatedKept{bf16_at(workspace, 0), nullptr, nullptr, nullptr};
+  if (keeps_rest(T)) kept.rest = bf16_at(workspace, hidden_bytes(L, T));
+  float* part = reinterpret_cast<float*>(bf16_at(workspace, forward_planes(L, T)));
   return launched(launch_gated_forward(gated_layer(L), static_cast<const uint16_t*>(x), T, static_cast<uint16_t*>(y), kept, part,
                                        static_cast<hipStream_t>(stream)));
 }
 
 size_t hire_gated_ffn_backward_workspace_bytes(const hire_gated_layer* L, int T) {
   if (check_gated(L, T) != HIRE_OK) return 0;
-  return 2 * hidden_bytes(L, T) + align_up(gated_backward_part_bytes(T, L->d_model, L->d_ff));
+  return backward_planes(L, T) + align_up(gated_backward_part_bytes(T, L->d_model, L->d_ff));
 }
 
 int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, const void* saved, const void* dy, void* dx,
@@ -120,11 +125,17 @@ int hire_gated_ffn_backward(const hire_gated_layer* L, const void* x, int T, con
     return HIRE_EINVAL;
   if (workspace_bytes < hire_gated_ffn_backward_workspace_bytes(L, T)) return HIRE_ENOSPC;
   const size_t hidden = hidden_bytes(L, T);
+  GatedSlopes slopes{bf16_at(workspace, 0), bf16_at(workspace, hidden)};
+  if (keeps_rest(T)) {
+    slopes.dg_rest = bf16_at(workspace, 2 * hidden);
+    slopes.du_rest = bf16_at(workspace, 3 * hidden);
+    slopes.h_rest = bf16_at(workspace, 4 * hidden);
+  }
   return launched(launch_gated_backward(
       gated_layer(L), static_cast<const uint16_t*>(x), T, kept_planes(L, T, const_cast<void*>(saved)),
       static_cast<const uint16_t*>(dy), static_cast<uint16_t*>(dx), static_cast<uint16_t*>(dwg), static_cast<uint16_t*>(dwu),
-      static_cast<uint16_t*>(dw2u), bf16_at(workspace, 0), bf16_at(workspace, hidden),
-      reinterpret_cast<float*>(bf16_at(workspace, 2 * hidden)), static_cast<hipStream_t>(stream)));
+      static_cast<uint16_t*>(dw2u), slopes, reinterpret_cast<float*>(bf16_at(workspace, backward_planes(L, T))),
+      static_cast<hipStream_t>(stream)));
 }
 
 int hire_pack_mxfp4(const void* w_bf16, int rows, int cols, void* codes, void* scales, void* stream) {

@@ -53,13 +53,37 @@ __device__ __forceinline__ void unpack_kept(const uint4& g, const uint4& u, cons
   }
 }
 
+// Values in two bf16 terms (kGatedRestTokens).  What the rounding leaves: 0 where the rounded value is no number or infinite.
+constexpr float kLargestFloat = 3.4028234663852886e38f;
+__device__ __forceinline__ float rest_of(float v, float rounded) {
+  const float rest = v - rounded;
+  return fabsf(rest) <= kLargestFloat ? rest : 0.0f;
+}
+__device__ __forceinline__ float bf16_rest(float v) { return rest_of(v, (float)(__bf16)v); }
+// A sum of both terms' products that is not finite is to be that of the first terms alone: the second terms' may be infinite on the
+// other side, or no number where an infinite factor meets a rest of 0.
+__device__ __forceinline__ float first_term(float both, float first) { return fabsf(both) <= kLargestFloat ? both : first; }
+template <int N>
+__device__ __forceinline__ bool all_finite(const float (&v)[N]) {
+  float zero = 0.0f;  // 0 times an infinity, or no number, is no number
+#pragma unroll
+  for (int e = 0; e < N; ++e) zero = fmaf(v[e], 0.0f, zero);
+  return zero == 0.0f;
+}
+
 // h = a(g) u of eight units, and what the backward pass needs (kept.g null: h only).
-template <int ACT>
+template <int ACT, bool REST = false>
 __device__ __forceinline__ void store_gated(const GatedKept& kept, size_t at, const float (&g)[8], const float (&u)[8]) {
   float hv[8], slope;
 #pragma unroll
   for (int e = 0; e < 8; ++e) hv[e] = activation<ACT>(g[e], &slope) * u[e];
   *reinterpret_cast<uint4*>(kept.h + at) = pack8(hv);
+  if constexpr (REST)
+    if (kept.rest) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) hv[e] = bf16_rest(hv[e]);
+      *reinterpret_cast<uint4*>(kept.rest + at) = pack8(hv);
+    }
   if (kept.g) {
     uint32_t gd[4], ud[4], low[4];
 #pragma unroll
@@ -80,7 +104,7 @@ __global__ __launch_bounds__(256) void k_join_gated(const float* __restrict__ pa
     float g[8], u[8];
     join_eight(part + i, parts, 2 * (size_t)values, g);
     join_eight(part + values + i, parts, 2 * (size_t)values, u);
-    store_gated<ACT>(kept, (size_t)i, g, u);
+    store_gated<ACT, true>(kept, (size_t)i, g, u);
   }
 }
 
@@ -134,7 +158,12 @@ struct StoreBf16 {
     });
   }
 };
-hipError_t launch_gated_few_weights(const GemmArgs& g, const StoreBf16<true>& out, hipStream_t s);  // gated_few.hip: K up to 64
+// gated_few.hip: K up to 64; rest: of the products' first operands (null: none)
+struct GatedRests {
+  const uint16_t* of[3];
+};
+hipError_t launch_gated_few_weights(const GemmArgs& g, const GatedRests& rest, const StoreBf16<true>& out, hipStream_t s);
+hipError_t launch_gated_rest(const GatedLayer& L, int T, const GatedKept& kept, uint16_t* rest, hipStream_t s);  // of the kept h
 
 // Calls f with the activation as a type.
 template <typename F>

@@ -105,11 +105,24 @@ __device__ __forceinline__ void leave_slice(float* red, const f32x4v (&sums)[MAT
 #pragma unroll
     for (int t = 0; t < NT; ++t) *reinterpret_cast<f32x4v*>(red + ((m * NT + t) * 64 + lane_id()) * 4) = sums[m][t];
 }
+__device__ __forceinline__ void put_bf16(uint16_t* to, float v) {
+  const __bf16 b = (__bf16)v;
+  __builtin_memcpy(to, &b, 2);
+}
 __device__ __forceinline__ void keep_gated(const GatedKept& kept, size_t at, float g, float u) {
   kept.g[at] = (uint16_t)(__float_as_uint(g) >> 16);
   kept.u[at] = (uint16_t)(__float_as_uint(u) >> 16);
   kept.low[at] = (uint16_t)((__float_as_uint(g) >> 8 & 0xFFu) | (__float_as_uint(u) & 0xFF00u));
 }
+
+struct KeptValue {
+  uint16_t h, g, u, low;
+  __device__ __forceinline__ void load(const GatedKept& kept, size_t at) {
+    h = kept.h[at], g = kept.g[at], u = kept.u[at], low = kept.low[at];
+  }
+  __device__ __forceinline__ float gate() const { return __uint_as_float((uint32_t)g << 16 | (low & 0xFFu) << 8); }
+  __device__ __forceinline__ float up() const { return __uint_as_float((uint32_t)u << 16 | (low & 0xFF00u)); }
+};
 
 constexpr int kUpWaves = 4;
 
@@ -130,8 +143,9 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const 
         if (token >= T || f >= L.d_ff) return;
         const size_t at = (size_t)token * L.d_ff + f;
         float slope;
-        const __bf16 h = (__bf16)(activation_of(L.act, v[0], &slope) * v[1]);
-        __builtin_memcpy(kept.h + at, &h, 2);
+        const float h = activation_of(L.act, v[0], &slope) * v[1];
+        put_bf16(kept.h + at, h);
+        if (kept.rest) put_bf16(kept.rest + at, bf16_rest(h));
         if (kept.g) keep_gated(kept, at, v[0], v[1]);
       });
   }
@@ -140,9 +154,19 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_up(GatedLayer L, const 
 // The backward pass's first product: dh of the units, and from it and what was kept dg and du.
 template <int NT, int RU>
 __global__ __launch_bounds__(64 * kUpWaves) void k_gated_slopes(GatedLayer L, const uint16_t* __restrict__ dy, int T, GatedKept kept,
-                                                                uint16_t* __restrict__ dg, uint16_t* __restrict__ du) {
+                                                                GatedSlopes to) {
   __shared__ float red[kUpWaves * NT * 256];
   const int unit0 = blockIdx.x * 16 * RU;
+  // up to sixteen tokens, a value for each thread: asked for in front of the products
+  constexpr bool kAhead = NT == 1;
+  KeptValue ahead[RU];
+  if constexpr (kAhead) {
+#pragma unroll
+    for (int r = 0; r < RU; ++r) {
+      const int f = min(unit0 + 16 * r + ((int)threadIdx.x & 15), L.d_ff - 1), token = min((int)threadIdx.x >> 4, T - 1);
+      ahead[r].load(kept, (size_t)token * L.d_ff + f);
+    }
+  }
   f32x4v sums[RU][1][NT] = {};
   up_products<1, NT, RU, kUpWaves>(dy, T, L.d, L.d_ff, {L.w2u}, unit0, wave_id(), sums);
 #pragma unroll
@@ -155,15 +179,32 @@ __global__ __launch_bounds__(64 * kUpWaves) void k_gated_slopes(GatedLayer L, co
         const int f = unit0 + 16 * r + unit;
         if (token >= T || f >= L.d_ff) return;
         const size_t at = (size_t)token * L.d_ff + f;
-        const uint32_t low = kept.low[at];
-        const float gv = __uint_as_float((uint32_t)kept.g[at] << 16 | (low & 0xFFu) << 8);
-        const float uv = __uint_as_float((uint32_t)kept.u[at] << 16 | (low & 0xFF00u));
+        KeptValue k;
+        if constexpr (kAhead)
+          k = ahead[r];
+        else
+          k.load(kept, at);
         float slope;
-        const float a = activation_of(L.act, gv, &slope);
-        const __bf16 dgv = (__bf16)(dh[0] * uv * slope), duv = (__bf16)(dh[0] * a);
-        __builtin_memcpy(dg + at, &dgv, 2);
-        __builtin_memcpy(du + at, &duv, 2);
+        const float a = activation_of(L.act, k.gate(), &slope);
+        const float dg = dh[0] * k.up() * slope, du = dh[0] * a;
+        put_bf16(to.dg + at, dg);
+        put_bf16(to.du + at, du);
+        if (to.dg_rest) {
+          put_bf16(to.dg_rest + at, bf16_rest(dg));
+          put_bf16(to.du_rest + at, bf16_rest(du));
+          put_bf16(to.h_rest + at, rest_of(a * k.up(), bf16_lo(k.h)));
+        }
       });
+  }
+}
+
+// What the rounding left of the kept h, where no other kernel of the backward pass reads g and u.
+__global__ __launch_bounds__(256) void k_gated_rest(int act, int values, GatedKept kept, uint16_t* __restrict__ rest) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < values; i += gridDim.x * 256) {
+    KeptValue k;
+    k.load(kept, i);
+    float slope;
+    put_bf16(rest + i, rest_of(activation_of(act, k.gate(), &slope) * k.up(), bf16_lo(k.h)));
   }
 }
 
@@ -216,7 +257,7 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, cons
                                                               float* __restrict__ part) {
   constexpr int kSlices = kOneWaves / GROUPS, kUnits = 16 * GROUPS, kBlocks = (kUnits + 31) / 32;
   __shared__ float red[kOneWaves * 512];
-  __shared__ __align__(16) __bf16 hidden[16 * kBlocks * 32];
+  __shared__ __align__(16) __bf16 hidden[2][16 * kBlocks * 32];  // and what the rounding left
   const int lane = lane_id(), wave = wave_id(), unit0 = blockIdx.x * kUnits, end = min(unit0 + kUnits, L.d_ff);
   const int group = wave % GROUPS, columns = (L.d + 127) / 128;
   f32x4v products[1][2][1] = {};
@@ -226,20 +267,19 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, cons
 #pragma unroll
   for (int b = 0; b < kBlocks; ++b) load_rows(L.w2u, L.d, chunk_of(min(wave, columns - 1)), unit0 + 32 * b, end, rows[b]);
   leave_slice<2, 1>(red + (group * kSlices + wave / GROUPS) * 512, products[0]);
-  for (int i = threadIdx.x; i < 16 * kBlocks * 32; i += 64 * kOneWaves) hidden[i] = (__bf16)0.0f;
+  for (int i = threadIdx.x; i < 16 * kBlocks * 32; i += 64 * kOneWaves) hidden[0][i] = hidden[1][i] = (__bf16)0.0f;
   __syncthreads();
   for (int i = threadIdx.x; i < GROUPS * 256; i += 64 * kOneWaves)
     join_slices<2, 1, kSlices>(red + i / 256 * kSlices * 512, i % 256, [&](int unit, int token, const float (&v)[2]) {
       const int in = i / 256 * 16 + unit;
       if (token >= T || unit0 + in >= L.d_ff) return;
       float slope;
-      const __bf16 h = (__bf16)(activation<ACT>(v[0], &slope) * v[1]);
-      hidden[token * kBlocks * 32 + in] = h;
-      if (kept.g) {
-        const size_t at = (size_t)token * L.d_ff + unit0 + in;
-        __builtin_memcpy(kept.h + at, &h, 2);
-        keep_gated(kept, at, v[0], v[1]);
-      }
+      const float h = activation<ACT>(v[0], &slope) * v[1];
+      hidden[0][token * kBlocks * 32 + in] = (__bf16)h;
+      hidden[1][token * kBlocks * 32 + in] = (__bf16)bf16_rest(h);
+      const size_t at = (size_t)token * L.d_ff + unit0 + in;
+      put_bf16(kept.h + at, h);  // also for k_join_units
+      if (kept.g) keep_gated(kept, at, v[0], v[1]);
     });
   __syncthreads();
   for (int block = wave; block < columns; block += kOneWaves) {
@@ -247,9 +287,12 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, cons
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
       if (unit0 + 32 * b + 32 > end) mask_rows(unit0 + 32 * b, end, rows[b]);
-      const bf16x8v hf = *reinterpret_cast<const bf16x8v*>(hidden + ((lane & 15) * kBlocks + b) * 32 + 8 * (lane >> 4));
 #pragma unroll
-      for (int c = 0; c < 8; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hf, column_of(rows[b], c), acc[c], 0, 0, 0);
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8v hf = *reinterpret_cast<const bf16x8v*>(hidden[t] + ((lane & 15) * kBlocks + b) * 32 + 8 * (lane >> 4));
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hf, column_of(rows[b], c), acc[c], 0, 0, 0);
+      }
       if (block + kOneWaves < columns) load_rows(L.w2u, L.d, chunk_of(block + kOneWaves), unit0 + 32 * b, end, rows[b]);
     }
     const int col = 128 * block + 8 * (lane & 15);
@@ -265,8 +308,11 @@ __global__ __launch_bounds__(64 * kOneWaves) void k_gated_one(GatedLayer L, cons
   }
 }
 
-// Sum of many parts of few values: sixteen threads share four values, each adds every sixteenth part.
-__global__ __launch_bounds__(256) void k_join_units(const float* __restrict__ part, uint16_t* __restrict__ y, int parts, int quads) {
+// Sum of many parts of few values: sixteen threads share four values, each adds every sixteenth part.  A sum that is not finite is that
+// of the first terms alone (first_term), which the same threads then form from h and the rows.  In k_gated_one, which would have to
+// keep both terms' sums apart, or the rows, this took its registers beyond the 128 of the small layers: 7.3 -> 9.1 us.
+__global__ __launch_bounds__(256) void k_join_units(GatedLayer L, const float* __restrict__ part, const uint16_t* __restrict__ h,
+                                                    uint16_t* __restrict__ y, int parts, int quads) {
   __shared__ float4 sums[256];
   const int quad = blockIdx.x * 16 + (int)threadIdx.x % 16, at = min(quad, quads - 1);
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -275,15 +321,36 @@ __global__ __launch_bounds__(256) void k_join_units(const float* __restrict__ pa
     const float4 v = reinterpret_cast<const float4*>(part)[(size_t)r * quads + at];
     s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
   }
-  sums[threadIdx.x] = s;
-  __syncthreads();
-  if (threadIdx.x >= 16 || quad >= quads) return;
-  for (int r = 1; r < 16; ++r) {
-    const float4 v = sums[16 * r + threadIdx.x];
-    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+  auto join = [&](const float4& mine, float (&joined)[4]) {
+    sums[threadIdx.x] = mine;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    const float4* all = sums + threadIdx.x;
+    joined[0] = mine.x, joined[1] = mine.y, joined[2] = mine.z, joined[3] = mine.w;
+    for (int r = 1; r < 16; ++r) {
+      const float4 v = all[16 * r];
+      joined[0] += v.x, joined[1] += v.y, joined[2] += v.z, joined[3] += v.w;
+    }
+  };
+  float f[4];
+  join(s, f);
+  const bool mine = threadIdx.x < 16 && quad < quads;
+  if (__syncthreads_or(mine && !all_finite(f))) {
+    const int token = 4 * at / L.d, col = 4 * at % L.d;
+    s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int unit = (int)threadIdx.x / 16; unit < L.d_ff; unit += 16) {
+      const float hv = bf16_lo(h[(size_t)token * L.d_ff + unit]);
+      const uint2 row = *reinterpret_cast<const uint2*>(L.w2u + (size_t)unit * L.d + col);
+      s.x = fmaf(hv, bf16_lo(row.x), s.x), s.y = fmaf(hv, bf16_hi(row.x), s.y);
+      s.z = fmaf(hv, bf16_lo(row.y), s.z), s.w = fmaf(hv, bf16_hi(row.y), s.w);
+    }
+    float first[4];
+    join(s, first);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = first_term(f[e], first[e]);
   }
-  const float f[4] = {s.x, s.y, s.z, s.w};
-  reinterpret_cast<uint2*>(y)[quad] = pack4(f);
+  if (mine) reinterpret_cast<uint2*>(y)[quad] = pack4(f);
 }
 
 // Sixteens of units of a workgroup: a workgroup for every compute unit, but no more than are resident at once.  d = 2048, one
@@ -314,7 +381,8 @@ hipError_t launch_one(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y
     return launch(&k_gated_one<decltype(act)::value, GROUPS, kOneWaves>, dim3((unsigned)parts), dim3(64 * kOneWaves), 0, s, L, x, T, kept, part);
   });
   return e != hipSuccess ? e
-                         : launch(&k_join_units, dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, part, y, parts, quads);
+                         : launch(&k_join_units, dim3((unsigned)((quads + 15) / 16)), dim3(256), 0, s, L, part, kept.h, y, parts,
+                                  quads);
 }
 
 // out = the sum over the pairs' rows, in parts where they are many.
@@ -336,24 +404,27 @@ hipError_t launch_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y
   const hipError_t e = few_streams(L.d, L.d_ff) ? launch_gated_stream(L, x, T, kept, part, s)
                                                : launch(&k_gated_up<NT, RU>, dim3((unsigned)((L.d_ff + 16 * RU - 1) / (16 * RU))),
                                                         dim3(64 * kUpWaves), 0, s, L, x, T, kept);
-  return e != hipSuccess ? e : launch_down(GatedDown{{L.w2u, nullptr}, {kept.h, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
+  if (e != hipSuccess) return e;
+  return launch_down(GatedDown{{L.w2u, nullptr}, {kept.h, nullptr}, {kept.rest, nullptr}, 1}, T, L.d, L.d_ff, y, part, s);
 }
 
 template <int NT>
-hipError_t launch_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+hipError_t launch_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, const GatedSlopes& slopes,
                          hipStream_t s) {
   const int groups = (L.d_ff + 15) / 16;
   if (groups >= 2 * 256)
-    return launch(&k_gated_slopes<NT, 2>, dim3((unsigned)((groups + 1) / 2)), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
-  return launch(&k_gated_slopes<NT, 1>, dim3((unsigned)groups), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, dg, du);
+    return launch(&k_gated_slopes<NT, 2>, dim3((unsigned)((groups + 1) / 2)), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, slopes);
+  return launch(&k_gated_slopes<NT, 1>, dim3((unsigned)groups), dim3(64 * kUpWaves), 0, s, L, dy, T, kept, slopes);
 }
 
 // ---- the weights' gradients -------------------------------------------------------------------
 // out[f, c] = sum over the tokens of a[token, f] b[token, c], bound by writing it.  A workgroup has both operands of its 128 x 128
 // tile in LDS as a whole (32 tokens STEPS times), so little of it that four share a compute unit and fill each other's waits.  d =
 // 2048, 16384 units, one token, us of the three: 75 as tiles of the many tokens' kernel, 60 this way, 36 with streaming stores.
-template <int STEPS>
-__global__ __launch_bounds__(256) void k_gated_outer(GemmArgs g, StoreBf16<true> out) {
+//   REST, up to sixteen tokens: a's second terms are k 16 ... of the one stage, with the same tokens of b.
+template <int STEPS, bool REST>
+__global__ __launch_bounds__(256) void k_gated_outer(GemmArgs g, GatedRests rest, StoreBf16<true> out) {
+  static_assert(!REST || (STEPS == 1 && kGatedRestTokens == 16), "two terms of sixteen tokens in a stage");
   using Tile = GemmTile<128, 4, false, false>;
   constexpr int kTiles = 2 * STEPS * Tile::kBytes, kRows = 4 * 32 * kRowFloats * 4;
   __shared__ __align__(1024) char smem[kTiles > kRows ? kTiles : kRows];
@@ -366,8 +437,20 @@ __global__ __launch_bounds__(256) void k_gated_outer(GemmArgs g, StoreBf16<true>
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(gemm_lds_offset(smem));
   const char* a = static_cast<const char*>(g.a[product]) + 2 * (size_t)m0;
   const char* b = static_cast<const char*>(g.b[product]) + 2 * (size_t)n0;
+  if constexpr (REST) {
+    const char* r = reinterpret_cast<const char*>(rest.of[product]) + 2 * (size_t)m0;
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
+    for (int i = 0; i < Tile::kLoads; ++i) {
+      const int piece = i * 4 + wave, k = Tile::k_of_lane(piece);
+      const bool there = (k & 15) < g.K;
+      const char* from_a = (k < 16 ? a : r) + (ta.off[i] - (uint32_t)(k & 16) * g.lda);
+      const char* from_b = b + (tb.off[i] - (uint32_t)(k & 16) * g.ldb);
+      gemm_load_at(there ? (const void*)from_a : (const void*)kGemmZeros, lds0 + piece * 1024);
+      gemm_load_at(there ? (const void*)from_b : (const void*)kGemmZeros, lds0 + Tile::kBytes + piece * 1024);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < (REST ? 0 : STEPS); ++s) {
     const int k = s * kGemmStep;
     ta.request(a + (size_t)k * g.lda, nullptr, g.K - k, lds0 + 2 * s * Tile::kBytes, wave);
     tb.request(b + (size_t)k * g.ldb, nullptr, g.K - k, lds0 + (2 * s + 1) * Tile::kBytes, wave);
@@ -391,7 +474,29 @@ __global__ __launch_bounds__(256) void k_gated_outer(GemmArgs g, StoreBf16<true>
         for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
     }
   lds_barrier();  // LDS is the epilogue's
-  out.store(acc, smem, m0 + wm, n0 + wn, g.M, g.N, product, 0);
+  if constexpr (REST) {
+    for_rows<false>(acc, smem, m0 + wm, n0 + wn, g.M, g.N, NoFetch{}, [&](int m, int n, const float (&sums)[1][8], int) {
+      uint16_t* to = out.c[product] + (size_t)m * g.N + n;
+      store_streaming(to, pack8(sums[0]));
+      if (all_finite(sums[0])) return;
+      uint32_t other = 0u;  // columns that are the first terms' (a loop, for little code)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) other |= (fabsf(sums[0][e]) <= kLargestFloat ? 0u : 1u) << e;
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        if ((other >> e & 1u) == 0u) continue;
+        const uint16_t* of_a = static_cast<const uint16_t*>(g.a[product]) + m;
+        const uint16_t* of_b = static_cast<const uint16_t*>(g.b[product]) + n + e;
+        float first = 0.0f;
+#pragma unroll 1
+        for (int k = 0; k < g.K; ++k)
+          first = fmaf(bf16_lo(of_a[(size_t)k * (g.lda / 2)]), bf16_lo(of_b[(size_t)k * (g.ldb / 2)]), first);
+        put_bf16(to + e, first);
+      }
+    });
+  } else {
+    out.store(acc, smem, m0 + wm, n0 + wn, g.M, g.N, product, 0);
+  }
 }
 
 // f with the number of tiles of sixteen tokens as a type.
@@ -440,23 +545,29 @@ hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint1
   });
 }
 
-hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, const GatedSlopes& slopes,
                                    float* part, hipStream_t s) {
   // streamed or not, us of this and dx: 17 / 64 tokens, d = 2560, 10240 units 45.7 / 57.8, 51.0 / 72.0, 8192, 2048 32.4 / 40.9, 38.3 /
   // 64.6, 2048, 16384 50.3 / 64.2, 52.6 / 69.9; sixteen 48.6, 47.6; of 1024, 8192 23.9 / 35.5, 22.2 / 30.7
   if (T > 16 && few_streams(L.d, L.d_ff) && (long long)L.d * L.d_ff >= 1 << 24)
-    return launch_gated_stream_slopes(L, dy, T, kept, dg, du, part, s);
-  return with_tiles(T, [&](auto tiles) { return launch_slopes<decltype(tiles)::value>(L, dy, T, kept, dg, du, s); });
+    return launch_gated_stream_slopes(L, dy, T, kept, slopes.dg, slopes.du, part, s);
+  return with_tiles(T, [&](auto tiles) { return launch_slopes<decltype(tiles)::value>(L, dy, T, kept, slopes, s); });
 }
 
-hipError_t launch_gated_few_weights(const GemmArgs& g, const StoreBf16<true>& out, hipStream_t s) {
+hipError_t launch_gated_few_weights(const GemmArgs& g, const GatedRests& rest, const StoreBf16<true>& out, hipStream_t s) {
   const long long tiles = (long long)((g.M + 127) / 128) * ((g.N + 127) / 128) * g.products;
-  return launch(g.K <= kGemmStep ? &k_gated_outer<1> : &k_gated_outer<2>, dim3((unsigned)tiles), dim3(256), 0, s, g, out);
+  const auto kernel = rest.of[0] ? &k_gated_outer<1, true> : (g.K <= kGemmStep ? &k_gated_outer<1, false> : &k_gated_outer<2, false>);
+  return launch(kernel, dim3((unsigned)tiles), dim3(256), 0, s, g, rest, out);
 }
 
-hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
-                               hipStream_t s) {
-  return launch_down(GatedDown{{L.wg, L.wu}, {dg, du}, 2}, T, L.d, L.d_ff, dx, part, s);
+hipError_t launch_gated_rest(const GatedLayer& L, int T, const GatedKept& kept, uint16_t* rest, hipStream_t s) {
+  const int values = T * L.d_ff;
+  return launch(&k_gated_rest, dim3(join_blocks(values)), dim3(256), 0, s, L.act, values, kept, rest);
+}
+
+hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const GatedSlopes& slopes, uint16_t* dx, float* part, hipStream_t s) {
+  return launch_down(GatedDown{{L.wg, L.wu}, {slopes.dg, slopes.du}, {slopes.dg_rest, slopes.du_rest}, 2}, T, L.d, L.d_ff, dx, part,
+                     s);
 }
 
 }  // namespace hire

@@ -101,12 +101,13 @@ hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, u
 }
 
 hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
-                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
-                                 float* part, hipStream_t s) {
+                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, const GatedSlopes& slopes, float* part,
+                                 hipStream_t s) {
+  uint16_t *const dg = slopes.dg, *const du = slopes.du;
   hipError_t e = hipSuccess;
   const bool few = T <= kGatedFewTokens;
   if (few && (dx || dwg || dwu)) {
-    e = launch_gated_few_slopes(L, dy, T, kept, dg, du, part, s);
+    e = launch_gated_few_slopes(L, dy, T, kept, slopes, part, s);
   } else if (dx || dwg || dwu) {
     GemmArgs a{};
     a.a[0] = dy, a.b[0] = L.w2u;
@@ -123,24 +124,27 @@ hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, 
         return launch(&k_join_slopes<ACT>, dim3(join_blocks(units / 8)), dim3(256), 0, s, part, shape.splits, units, kept, dg, du);
       return launch_product<true, true, false, false>(a, shape.tile, StoreGateSlopes<ACT>{kept, dg, du}, s);
     });
+  } else if (slopes.h_rest) {
+    e = launch_gated_rest(L, T, kept, slopes.h_rest, s);
   }
   if (e != hipSuccess) return e;
   GemmArgs w{};
+  GatedRests rest{};
   StoreBf16<true> out{};
-  auto add = [&](const uint16_t* a, const uint16_t* b, uint16_t* c) {
-    if (c) w.a[w.products] = a, w.b[w.products] = b, out.c[w.products++] = c;
+  auto add = [&](const uint16_t* a, const uint16_t* a_rest, const uint16_t* b, uint16_t* c) {
+    if (c) w.a[w.products] = a, rest.of[w.products] = a_rest, w.b[w.products] = b, out.c[w.products++] = c;
   };
-  add(dg, x, dwg);
-  add(du, x, dwu);
-  add(kept.h, dy, dw2u);
+  add(dg, slopes.dg_rest, x, dwg);
+  add(du, slopes.du_rest, x, dwu);
+  add(kept.h, slopes.h_rest, dy, dw2u);
   if (w.products > 0) {
     w.M = L.d_ff, w.N = L.d, w.K = T, w.lda = 2u * L.d_ff, w.ldb = 2u * L.d;
     w.segments = w.splits = 1;
-    e = few ? launch_gated_few_weights(w, out, s)
+    e = few ? launch_gated_few_weights(w, rest, out, s)
             : launch_split_products<false, false>(w, weights_shape(T, L.d, L.d_ff, w.products), out, part, s);
     if (e != hipSuccess) return e;
   }
-  if (dx && few) return launch_gated_few_dx(L, T, dg, du, dx, part, s);
+  if (dx && few) return launch_gated_few_dx(L, T, slopes, dx, part, s);
   if (dx) {
     GemmArgs a{};
     a.a[0] = dg, a.a[1] = du, a.b[0] = L.wg, a.b[1] = L.wu;

@@ -132,15 +132,20 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
         const size_t at = (size_t)token * L.d_ff + unit;
         const f32x4v g = v[0], u = v[1];
         if (part) {
-          float* to = part + 2 * blockIdx.y * units + at;
-          *reinterpret_cast<f32x4v*>(to) = g;
-          *reinterpret_cast<f32x4v*>(to + units) = u;
+          float* sums = part + 2 * blockIdx.y * units + at;
+          *reinterpret_cast<f32x4v*>(sums) = g;
+          *reinterpret_cast<f32x4v*>(sums + units) = u;
           return;
         }
         float h[4], slope;
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = activation_of(L.act, g[e], &slope) * u[e];
         *reinterpret_cast<uint2*>(kept.h + at) = pack4(h);
+        if constexpr (NT == 1) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = bf16_rest(h[e]);
+          *reinterpret_cast<uint2*>(kept.rest + at) = pack4(h);
+        }
         if (kept.g) {
           *reinterpret_cast<uint2*>(kept.g + at) = make_uint2(upper_pair(g[0], g[1]), upper_pair(g[2], g[3]));
           *reinterpret_cast<uint2*>(kept.u + at) = make_uint2(upper_pair(u[0], u[1]), upper_pair(u[2], u[3]));
@@ -221,7 +226,10 @@ constexpr int kDownRows = 32, kDownCols = 128, kDownMatrix = kDownRows * kDownCo
 template <int NT>
 __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_gated_down_stream(
     GatedDown from, int T, int d, int d_ff, float* __restrict__ part, uint16_t* __restrict__ y) {
-  constexpr int kPlaces = NT <= 2 ? 4 : 3, kPlace = kDownMatrix + NT * 1024, kBlocks = kDownCols / 16;
+  constexpr bool REST = NT == 1;  // two terms of the tokens' values
+  static_assert(kGatedRestTokens == 16, "one sixteen");
+  constexpr int kTerms = REST ? 2 : 1, kPlaces = NT * kTerms <= 2 ? 4 : 3, kPlace = kDownMatrix + NT * kTerms * 1024;
+  constexpr int kBlocks = kDownCols / 16;
   __shared__ __align__(1024) char smem[kStreamWaves * kPlaces * kPlace];
   static_assert(sizeof(smem) >= kStreamWaves * NT * 16 * kDownCols * 4, "the sums");
   const int wave = __builtin_amdgcn_readfirstlane(wave_id()), lane = lane_id(), r = lane & 15, q = lane >> 4;
@@ -247,13 +255,16 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
 #pragma unroll
     for (int t = 0; t < NT; ++t) {  // sixteen tokens; chunk c of token m lies at c ^ (m / 4 % 4)
       const int token = lane >> 2, chunk = (lane & 3) ^ (token >> 2);
-      const uint16_t* h = from.h[pair] + (size_t)min(16 * t + token, T - 1) * d_ff + k0 + 8 * chunk;
-      gemm_load_at(k0 + 8 * chunk < d_ff ? (const void*)h : (const void*)kGemmZeros, lds + kDownMatrix + t * 1024);
+      const size_t at = (size_t)min(16 * t + token, T - 1) * d_ff + k0 + 8 * chunk;
+      const bool there = k0 + 8 * chunk < d_ff;
+      gemm_load_at(there ? (const void*)(from.h[pair] + at) : (const void*)kGemmZeros, lds + kDownMatrix + t * 1024);
+      if constexpr (REST)
+        gemm_load_at(there ? (const void*)(from.rest[pair] + at) : (const void*)kGemmZeros, lds + kDownMatrix + (NT + t) * 1024);
     }
   };
-  constexpr int kLoads = kDownLoads + NT;
+  constexpr int kLoads = kDownLoads + NT * kTerms;
   for (int i = 0; i < kPlaces - 1 && i < n; ++i) request(i);
-  f32x4v acc[NT][kBlocks] = {};
+  f32x4v acc[NT * kTerms][kBlocks] = {};
   for (int i = 0; i < n; ++i) {
     if (i + kPlaces - 2 < n)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kPlaces - 2) * kLoads) : "memory");
@@ -263,9 +274,9 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     if (i + kPlaces - 1 < n) request(i + kPlaces - 1);  // where the block before was
     const char* place = smem + (wave * kPlaces + i % kPlaces) * kPlace;
-    bf16x8v hf[NT];
+    bf16x8v hf[NT * kTerms];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT * kTerms; ++t)
       hf[t] = *reinterpret_cast<const bf16x8v*>(place + kDownMatrix + t * 1024 + r * 64 + ((q ^ (r >> 2)) << 4));
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
@@ -278,8 +289,15 @@ __global__ __launch_bounds__(64 * kStreamWaves) __attribute__((amdgpu_waves_per_
       __builtin_memcpy(&col, &lo, 8);
       __builtin_memcpy(reinterpret_cast<char*>(&col) + 8, &hi, 8);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, hf[t], acc[t][c], 0, 0, 0);
+      for (int t = 0; t < NT * kTerms; ++t) acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(col, hf[t], acc[t][c], 0, 0, 0);
     }
+  }
+  if constexpr (REST) {
+    // the first terms' sum stays as it is where it is not finite (gated.h, first_term)
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][c][e] += fabsf(acc[0][c][e]) <= kLargestFloat ? acc[1][c][e] : 0.0f;
   }
   // acc[t][c]: token 16 t + lane % 16, columns 16 c + 4 q ...; the waves' sums are added in their order
   __syncthreads();

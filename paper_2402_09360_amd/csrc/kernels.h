@@ -482,19 +482,32 @@ struct GatedLayer {
 // Bytes of the fp32 parts of the products that are split; 0: none is.
 size_t gated_forward_part_bytes(int T, int d, int d_ff);
 size_t gated_backward_part_bytes(int T, int d, int d_ff);
-// Planes [T, d_ff] of 16 bits that the forward pass leaves for the backward pass; g, u, low null: h only.
+// Planes [T, d_ff] of 16 bits that the forward pass leaves for the backward pass; g, u, low null: h only.  rest (up to
+// kGatedRestTokens tokens, not kept): what rounding h to bf16 leaves of it.
 struct GatedKept {
-  uint16_t *h, *g, *u, *low;
+  uint16_t *h, *g, *u, *low, *rest = nullptr;
+};
+// dg and du [T, d_ff] in bf16; up to kGatedRestTokens tokens also what the rounding leaves of them and of the kept h (else null).
+struct GatedSlopes {
+  uint16_t *dg, *du, *dg_rest = nullptr, *du_rest = nullptr, *h_rest = nullptr;
 };
 hipError_t launch_gated_forward(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                                 hipStream_t s);
-// dx, dwg, dwu, dw2u: any may be null; dg, du [T, d_ff] scratch.
+// dx, dwg, dwu, dw2u: any may be null; slopes: scratch.
 hipError_t launch_gated_backward(const GatedLayer& L, const uint16_t* x, int T, const GatedKept& kept, const uint16_t* dy,
-                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, uint16_t* dg, uint16_t* du,
-                                 float* part, hipStream_t s);
+                                 uint16_t* dx, uint16_t* dwg, uint16_t* dwu, uint16_t* dw2u, const GatedSlopes& slopes, float* part,
+                                 hipStream_t s);
 
 // ---- gated_few.hip: up to kGatedFewTokens tokens; the backward pass's dg and du, and dx from them
 constexpr int kGatedFewTokens = 64;
+// Up to so many tokens h, dg and du go into the products that follow as two bf16 terms, rounded and what the rounding left: sixteen
+// bits of significand, so that results are rounded once and no more.  In one term they are off by as much as a result's own rounding
+// (errors of 0.0024 instead of 0.0017 of the norm; of few values up to 0.003).  Those products are bound by reading the matrices or
+// writing their gradients; us, forward / backward, one term and two: d = 2048, 16384 units, one token 35.2, 35.7 / 82.8, 83.2, sixteen
+// 49.1, 49.5 / 89.8, 88.0; 256, 1024, one 7.3, 7.4 / 12.6, 13.5; 1024, 4096, sixteen 14.8, 15.5 / 22.5, 23.5.  With more tokens, y and dx
+// alone: 17 to 32 up to 5 and 6 % longer, 33 to 64 up to 8 and 9 (the rests take LDS from the rows on their way); many tokens would
+// have twice the matrix instructions in those products.
+constexpr int kGatedRestTokens = 16;
 size_t gated_few_part_bytes(int T, int d, int d_ff, int pairs);  // pairs: 1 forward, 2 dx
 hipError_t launch_gated_few(const GatedLayer& L, const uint16_t* x, int T, uint16_t* y, const GatedKept& kept, float* part,
                             hipStream_t s);
@@ -504,15 +517,14 @@ hipError_t launch_gated_stream(const GatedLayer& L, const uint16_t* x, int T, co
 hipError_t launch_gated_stream_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
                                       float* part, hipStream_t s);
 struct GatedDown {
-  const uint16_t *w[2], *h[2];  // a matrix and its values, or two pairs whose products are added
-  int pairs;
+  const uint16_t *w[2], *h[2], *rest[2];  // a matrix and its values (rest: null, or what their rounding left), or two pairs whose
+  int pairs;                              // products are added
 };
 hipError_t launch_gated_down_stream(const GatedDown& from, int T, int d, int d_ff, int parts, uint16_t* out, float* part,
                                     hipStream_t s);
-hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, uint16_t* dg, uint16_t* du,
+hipError_t launch_gated_few_slopes(const GatedLayer& L, const uint16_t* dy, int T, const GatedKept& kept, const GatedSlopes& slopes,
                                    float* part, hipStream_t s);
-hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const uint16_t* dg, const uint16_t* du, uint16_t* dx, float* part,
-                               hipStream_t s);
+hipError_t launch_gated_few_dx(const GatedLayer& L, int T, const GatedSlopes& slopes, uint16_t* dx, float* part, hipStream_t s);
 
 // ---- mxfp4.hip: microscaled 4-bit floating point ---------------------------------
 hipError_t launch_pack_mxfp4(const uint16_t* w, int rows, int cols, uint8_t* codes, uint8_t* scales, hipStream_t s);
