@@ -335,7 +335,11 @@ __global__ __launch_bounds__(256) void k_join_units(GatedLayer L, const float* _
   float f[4];
   join(s, f);
   const bool mine = threadIdx.x < 16 && quad < quads;
-  if (__syncthreads_or(mine && !all_finite(f))) {
+  const uint64_t others = __ballot(mine && !all_finite(f));  // the first wave's
+  __shared__ int again;
+  if (threadIdx.x == 0) again = others != 0ull;
+  __syncthreads();
+  if (again) {
     const int token = 4 * at / L.d, col = 4 * at % L.d;
     s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
