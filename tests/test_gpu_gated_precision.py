@@ -21,7 +21,7 @@ def hire():
                                        (12, 8192, 4104, "silu"), (1, 2048, 20000, "gelu")])
 def test_rounded_once(hire, T, d, F, act):
     """Rounded to one bf16 term, h (or dg and du) is off by about 0.4 2^-8 of its value, and so is a sum of many, while a result's
-    rounding step is 2^-8 to 2^-7 of it: about every fourth result would come out as a neighbour.  Two terms, and g and u kept in 24
+    rounding step is 2^-8 to 2^-7 of it: a quarter to two fifths of the results would come out as a neighbour.  Two terms, and g and u kept in 24
     bits, are off by 2^-15 at most: less than one in a hundred.  Two in a hundred are allowed."""
     print(T, d, F, act, flush=True)
     wrong = dict(y=0, dx=0, dwg=0, dwu=0, dw2u=0)
